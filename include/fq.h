@@ -264,6 +264,129 @@ size_t fq_gptq_sweep_workspace_bytes(int64_t N, int64_t K);
 fq_status fq_gptq_sweep(const float *w_t, int64_t ldw, const double *U, int64_t N, int64_t K, int b, int bits,
                         int8_t *w_codes, float *w_scale, void *ws, size_t ws_bytes, void *stream);
 
+/* ---- Attention between the projections -----------------------------------------------------
+ * The operators that turn one site's q|k|v projection into the next site's input: norms of
+ * queries and keys per head and the position rotation, a paged cache of keys and values in 8
+ * bits, attention over that cache, and attention to another sequence's states.
+ *   fq_rope_table       cos/sin of every position, once per model
+ *   fq_qk_rope          norm and rotation of queries and keys
+ *   fq_cache_append     the same, with keys and values rounded into the cache
+ *   fq_cache_read       tokens of the cache as values
+ *   fq_cache_attention  attention over the cache
+ *   fq_cross_attention  attention to bf16 keys and values of another length
+ * Shapes: query heads Hq, key heads Hk with Hq a multiple of Hk (query head h reads key head
+ * h / (Hq / Hk)), both at most 1024; head size D a multiple of 16 in [16, 256]; the rotary part R a multiple of 16,
+ * 0 <= R <= D.  Queries, keys and values are bf16; statistics, softmax and sums are fp32. */
+
+/* bf16 rows of heads: element d of head h of token t (of sequence b) at
+ * p[b batch_stride + t token_stride + h head_stride + d], strides in elements, multiples of
+ * 8 and at least 0 (a stride is not looked at where its count is 1). */
+typedef struct {
+  const void *p;
+  int64_t batch_stride, token_stride, head_stride;
+} fq_heads;
+
+/* Norm and rotation of a head x of a token at position m:
+ *   y = x rsqrt(mean x^2 + eps) w   where w is given (fp32 [D]; NULL: y = x)
+ *   pair (a, b) of y -> (a c - b s, b c + a s), (c, s) = table[m][i], for the R/2 pairs i:
+ *   dims (i, i + R/2), or (2i, 2i + 1) where `interleaved`; dims from R on stay.
+ *   table      fp32 [length, R/2, 2], 8-byte pairs cos, sin (fq_rope_table); NULL: R = 0.
+ *   positions  int32, one per token, or NULL (fq_qk_rope: the token's index; fq_cache_append:
+ *              the token's place in its sequence).  A position outside [0, length) is
+ *              clamped into it. */
+typedef struct {
+  const float *table;
+  int64_t length;
+  const int32_t *positions;
+  const float *q_weight, *k_weight;
+  float eps;
+  int32_t rot;
+  int32_t interleaved;
+  int32_t reserved;
+} fq_head_rope;
+
+/* A pool of cache pages, P tokens each (P = 16, 32, 64 or 128), one scale per page and head:
+ *   k_codes  int8 [pages, heads, P, D]         k_scale  fp32 [pages, heads]
+ *   v_codes  int8 [pages, heads, P/16, D, 16]  v_scale  fp32 [pages, heads]
+ * (the tokens of a group of 16 are adjacent in v_codes: the order in which the product with
+ * the attention weights sums them).  A value is code * scale. */
+typedef struct {
+  void *k_codes;
+  float *k_scale;
+  void *v_codes;
+  float *v_scale;
+  int64_t pages;
+  int32_t heads, page_tokens, head_dim, reserved;
+} fq_kv_cache;
+
+/* A ragged batch of sequences over a cache, all int32 device arrays (4-byte aligned, as
+ * every index array of these entry points):
+ *   q_start     [seqs + 1]: the tokens of sequence b are rows q_start[b] .. q_start[b+1] - 1
+ *   kv_len      [seqs]: tokens of the sequence in the cache, the call's own included (a
+ *               sequence's last n tokens are its rows of this call)
+ *   page_table  [seqs, table_width]: page of tokens P w .. P w + P - 1 of the sequence
+ * max_new and max_kv are bounds of the rows of a sequence and of kv_len, known to the host;
+ * rows and tokens beyond them are not computed or seen.  table_width * P >= max_kv.  An
+ * entry outside the pool is clamped into it.  Pages in use by two sequences may be read, not appended to. */
+typedef struct {
+  const int32_t *q_start, *kv_len, *page_table;
+  int64_t table_width, seqs, max_new, max_kv;
+} fq_kv_batch;
+
+/* table[m][i] = magnitude * (cos, sin)(m inv_freq[i]) for m < length: angles in fp64 (a
+ * position of 10^5 times a frequency near 1 keeps its fraction), rounded once to fp32.
+ *   inv_freq  fp64 device [pairs]: radians per position; scalings for long contexts are
+ *   scalings of these and of `magnitude`. */
+fq_status fq_rope_table(const double *inv_freq, double magnitude, int64_t length, int64_t pairs, float *table,
+                        void *stream);
+
+/* q_out bf16 [T, Hq, D], k_out bf16 [T, Hk, D]: norm and rotation, fp32 inside, one rounding.
+ * k and k_out may be NULL (Hk = 0 then), and so may q and q_out (Hq = 0). */
+fq_status fq_qk_rope(const fq_heads *q, int Hq, const fq_heads *k, int Hk, const fq_head_rope *rope, int64_t T, int D,
+                     void *q_out, void *k_out, void *stream);
+
+/* Appends T tokens (all sequences of the batch) to the cache: token i of sequence b goes to
+ * slot kv_len[b] - n_b + i, its keys normed and rotated, its values as they are.  For every
+ * page and head that new tokens reach, with a = max |x| over them in fp32:
+ *   scale' = a / 127, or max(scale, a / 127) where the page holds earlier tokens;
+ *   earlier codes = rne(code * (scale / scale')) where the scale grew;
+ *   new codes = clamp(rne(x * (1 / scale')), -127, 127).
+ * A scale below the smallest normal fp32 is 0, its codes too.  A page given a value that is
+ * not finite gets the scale NaN: what attends to any of its tokens (of that head) is NaN.
+ * Slots of the page beyond the last token hold unspecified codes.
+ * q (or NULL, with Hq = 0 and q_out = NULL): normed and rotated into q_out [T, Hq, D] in the
+ * same launch.  rope may be NULL: no norm and no rotation.  T >= q_start[seqs]. */
+fq_status fq_cache_append(const fq_kv_cache *cache, const fq_kv_batch *batch, const fq_heads *k, const fq_heads *v,
+                          const fq_heads *q, int Hq, const fq_head_rope *rope, int64_t T, void *q_out, void *stream);
+
+/* k_out, v_out bf16 [seqs, max_tokens, heads, D]: tokens first[b] .. last[b] - 1 of every
+ * sequence (int32 device arrays), code * scale rounded once; zeros from last[b] - first[b]
+ * on.  Either output may be NULL. */
+fq_status fq_cache_read(const fq_kv_cache *cache, const int32_t *page_table, int64_t table_width,
+                        const int32_t *first, const int32_t *last, int64_t seqs, int64_t max_tokens, void *k_out,
+                        void *v_out, void *stream);
+
+/* out bf16 [T, Hq, D] = softmax(scale q k^T) v per row over the cache: row i of a sequence
+ * of n rows sees tokens j < kv_len, and j <= kv_len - n + i where `causal`.  A row that sees
+ * nothing gives zeros.  scale > 0.  ws: fq_cache_attention_workspace_bytes bytes (partial
+ * results where a sequence's tokens are split over workgroups; 0 and NULL where they are
+ * not), no initialization. */
+size_t fq_cache_attention_workspace_bytes(int64_t T, int Hq, int Hk, int D, int64_t seqs, int64_t max_new,
+                                          int64_t max_kv);
+fq_status fq_cache_attention(const fq_heads *q, int Hq, int64_t T, const fq_kv_cache *cache, const fq_kv_batch *batch,
+                             float scale, int causal, void *out, void *ws, size_t ws_bytes, void *stream);
+
+/* out bf16 [B, Sq, Hq, D] = softmax(scale q k^T) v over the Sk states of each sample.
+ *   kv_len    int32 [B] states in use of each sample, or NULL (all)
+ *   key_mask  uint8, place j of sample b at key_mask[b mask_stride + j], nonzero = seen, or
+ *             NULL; any alignment; mask_stride 0: one mask for all
+ * What lies in unseen places (NaN and infinities too) has no effect; a sample that sees
+ * nothing gives zeros.  ws: as above. */
+size_t fq_cross_attention_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, int Hq, int Hk, int D);
+fq_status fq_cross_attention(const fq_heads *q, const fq_heads *k, const fq_heads *v, const int32_t *kv_len,
+                             const uint8_t *key_mask, int64_t mask_stride, int64_t B, int64_t Sq, int64_t Sk, int Hq,
+                             int Hk, int D, float scale, void *out, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -3,14 +3,13 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <atomic>
 #include <cstring>
 #include <initializer_list>
 
 #include "../../include/fq.h"
 #include "fq_launch.hpp"
+#include "fq_status.hpp"
 
 // Scratch of fq_linear_static: the workspace of fq_linear in a file-scope device array
 // instead of a caller's buffer.  In host code `scratch` names a host-side stand-in, not the
@@ -20,51 +19,7 @@ static __device__ __align__(256) uint8_t scratch[kStaticScratchBytes];
 
 namespace {
 
-thread_local char g_err[512] = "";
-
-fq_status fail(fq_status s, const char *fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof g_err, fmt, ap);
-  va_end(ap);
-  return s;
-}
-
-fq_status ok() {
-  g_err[0] = '\0';
-  return FQ_OK;
-}
-
-fq_status hip_fail(hipError_t e, const char *where) {
-  return fail(FQ_ERR_HIP, "%s: %s", where, hipGetErrorString(e));
-}
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-bool is_pow2(int64_t v) { return v >= 1 && (v & (v - 1)) == 0; }
-
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-// Byte range [p, p + n) of a caller buffer, for the no-overlap preconditions.
-struct Span {
-  uintptr_t lo, hi;
-};
-Span span(const void *p, size_t n) { return Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + n}; }
-bool overlap(Span a, Span b) { return a.lo && b.lo && a.lo < b.hi && b.lo < a.hi; }
-// True when an output range overlaps another output or any input (NULL ranges are empty).
-bool outputs_alias(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
-  for (auto o = outs.begin(); o != outs.end(); ++o) {
-    for (auto p = o + 1; p != outs.end(); ++p)
-      if (overlap(*o, *p)) return true;
-    for (const Span &i : ins)
-      if (overlap(*o, i)) return true;
-  }
-  return false;
-}
-// Bytes spanned by `rows` rows of `row_bytes` bytes at a stride of `ld_bytes`.
-size_t rows_span(int64_t rows, int64_t ld_bytes, int64_t row_bytes) {
-  return rows <= 0 ? 0 : (size_t)(rows - 1) * (size_t)ld_bytes + (size_t)row_bytes;
-}
+using namespace fq;
 
 constexpr int64_t kMaxK = 32768;
 constexpr int64_t kMaxGptqK = 16384;  // the factor holds two K x K fp64 matrices

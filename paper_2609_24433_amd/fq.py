@@ -7,8 +7,10 @@ If libfq.so is missing the import fails loudly; there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
-from typing import Optional, Tuple
+import struct
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -26,6 +28,9 @@ EXPORTED = ["fq_fwht_quant", "fq_quantize_weights", "fq_packed_weight_bytes", "f
             "fq_transform", "fq_gptq_hessian", "fq_gptq_factor_workspace_bytes", "fq_gptq_factor",
             "fq_gptq_sweep_workspace_bytes", "fq_gptq_sweep",
             "fq_linear_static_max_workspace_bytes", "fq_linear_static",
+            "fq_rope_table", "fq_qk_rope", "fq_cache_append", "fq_cache_read",
+            "fq_cache_attention_workspace_bytes", "fq_cache_attention",
+            "fq_cross_attention_workspace_bytes", "fq_cross_attention",
             "fq_status_string", "fq_last_error"]
 
 
@@ -40,6 +45,8 @@ def _load() -> ctypes.CDLL:
         raise ImportError(f"{LIB_PATH} is not built; run __graft_entry__.build() "
                           "(python -m paper_2609_24433_amd.build)")
     lib = ctypes.CDLL(LIB_PATH)
+    # descriptors (fq_heads and its kin) come as packed bytes
+    desc = ctypes.c_char_p
     vp, i64, i32, f32, sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
     sig = {
         "fq_fwht_quant": [vp, i64, vp, vp, i64, i64, i32, i32, f32, vp, vp, vp],
@@ -57,6 +64,12 @@ def _load() -> ctypes.CDLL:
         "fq_gptq_factor": [vp, i64, ctypes.c_double, vp, vp, sz, vp],
         "fq_gptq_sweep": [vp, i64, vp, i64, i64, i32, i32, vp, vp, vp, sz, vp],
         "fq_linear_static": [vp, i64, vp, vp, i64, i64, i64, i32, i32, f32, vp, vp, vp, vp, i64, vp],
+        "fq_rope_table": [vp, ctypes.c_double, i64, i64, vp, vp],
+        "fq_qk_rope": [desc, i32, desc, i32, desc, i64, i32, vp, vp, vp],
+        "fq_cache_append": [desc, desc, desc, desc, desc, i32, desc, i64, vp, vp],
+        "fq_cache_read": [desc, vp, i64, vp, vp, i64, i64, vp, vp, vp],
+        "fq_cache_attention": [desc, i32, i64, desc, desc, f32, i32, vp, vp, sz, vp],
+        "fq_cross_attention": [desc, desc, desc, vp, vp, i64, i64, i64, i64, i32, i32, i32, f32, vp, vp, sz, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -69,7 +82,9 @@ def _load() -> ctypes.CDLL:
                        "fq_rotate_quant_workspace_bytes": [i64, i64],
                        "fq_gptq_factor_workspace_bytes": [i64],
                        "fq_gptq_sweep_workspace_bytes": [i64, i64],
-                       "fq_linear_static_max_workspace_bytes": []}.items():
+                       "fq_linear_static_max_workspace_bytes": [],
+                       "fq_cache_attention_workspace_bytes": [i64, i32, i32, i32, i64, i64, i64],
+                       "fq_cross_attention_workspace_bytes": [i64, i64, i64, i32, i32, i32]}.items():
         fn = getattr(lib, name)
         fn.argtypes = args
         fn.restype = sz
@@ -390,3 +405,230 @@ class QuantLinear:
                  post_inv: Optional[torch.Tensor] = None) -> torch.Tensor:
         return linear(x, self.w_packed, self.w_scale, self.N, self.b, self.bits, clip_ratio, smooth_inv,
                       self.bias, ws, out, post_inv)
+
+
+# ---------------------------------------------------------------- attention between the projections
+
+_HEADS = struct.Struct("=Qqqq").pack          # fq_heads
+_ROPE = struct.Struct("=QqQQQfiii").pack      # fq_head_rope
+_CACHE = struct.Struct("=QQQQqiiii").pack     # fq_kv_cache
+_BATCH = struct.Struct("=QQQqqqq").pack       # fq_kv_batch
+
+
+class KVCache(NamedTuple):
+    """Pages of keys and values in 8 bits, one scale per page and head (kv_cache makes them)."""
+    k_codes: torch.Tensor  # int8 [pages, heads, P, D]
+    k_scale: torch.Tensor  # fp32 [pages, heads]
+    v_codes: torch.Tensor  # int8 [pages, heads, P/16, D, 16]
+    v_scale: torch.Tensor  # fp32 [pages, heads]
+
+
+def kv_cache(pages: int, heads: int, page_tokens: int, head_dim: int, device="cuda") -> KVCache:
+    """A pool of empty cache pages of page_tokens = 16, 32, 64 or 128 tokens."""
+    return KVCache(torch.zeros((pages, heads, page_tokens, head_dim), dtype=torch.int8, device=device),
+                   torch.zeros((pages, heads), dtype=torch.float32, device=device),
+                   torch.zeros((pages, heads, page_tokens // 16, head_dim, 16), dtype=torch.int8, device=device),
+                   torch.zeros((pages, heads), dtype=torch.float32, device=device))
+
+
+def _ptr0(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def _heads(x: torch.Tensor, name: str) -> bytes:
+    _require(x.dtype == torch.bfloat16 and x.stride(-1) == 1, f"{name}: bf16 with unit stride of the last dim")
+    s = x.stride()
+    return _HEADS(x.data_ptr(), s[0] if len(s) == 4 else 0, s[-3], s[-2])
+
+
+def _index(t: Optional[torch.Tensor], n: int, name: str) -> int:
+    if t is None:
+        return 0
+    _require(t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == n and (n < 2 or t.stride(0) == 1),
+             f"{name}: contiguous int32 [{n}]")
+    return t.data_ptr()
+
+
+def _cache_desc(c: KVCache) -> Tuple[bytes, int, int]:
+    kc, ks, vc, vs = c
+    pages, H, P, D = kc.shape
+    _require(kc.dtype == torch.int8 and vc.dtype == torch.int8 and tuple(vc.shape) == (pages, H, P // 16, D, 16)
+             and kc.is_contiguous() and vc.is_contiguous(), "cache codes: contiguous int8 [pages, heads, P, D] and [pages, heads, P/16, D, 16]")
+    _require(ks.dtype == torch.float32 and vs.dtype == torch.float32 and tuple(ks.shape) == (pages, H)
+             and tuple(vs.shape) == (pages, H) and ks.is_contiguous() and vs.is_contiguous(),
+             "cache scales: contiguous fp32 [pages, heads]")
+    return _CACHE(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), pages, H, P, D, 0), H, D
+
+
+def _batch_desc(page_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, max_new: int, max_kv: int = 0,
+                page_tokens: int = 0) -> bytes:
+    """fq_kv_batch; page_tokens instead of max_kv: all tokens that the table holds."""
+    _require(page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous(),
+             "page_table: contiguous int32 [seqs, pages]")
+    B, width = page_table.shape
+    return _BATCH(_index(q_start, B + 1, "q_start"), _index(kv_len, B, "kv_len"), page_table.data_ptr(), width, B, max_new,
+                  max_kv or width * page_tokens)
+
+
+def _rope_desc(table, positions, T, q_weight, k_weight, D, eps, interleaved) -> bytes:
+    length = rot = 0
+    if table is not None:
+        _require(table.dtype == torch.float32 and table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous(),
+                 "table: contiguous fp32 [length, R/2, 2]")
+        length, rot = table.shape[0], 2 * table.shape[1]
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        _require(w is None or (w.dtype == torch.float32 and tuple(w.shape) == (D,) and w.is_contiguous()),
+                 f"{name}: contiguous fp32 [{D}]")
+    return _ROPE(_ptr0(table), length, _index(positions, T, "positions"), _ptr0(q_weight), _ptr0(k_weight), eps, rot,
+                 int(interleaved), 0)
+
+
+def _check_rows(out: Optional[torch.Tensor], like: torch.Tensor, name: str) -> torch.Tensor:
+    """A contiguous bf16 output of the shape of `like`, the caller's or a new one."""
+    if out is None:
+        return torch.empty(like.shape, dtype=torch.bfloat16, device=like.device)
+    _require(out.dtype == torch.bfloat16 and out.shape == like.shape and out.is_contiguous(),
+             f"{name}: contiguous bf16 {tuple(like.shape)}")
+    return out
+
+
+def rope_frequencies(rot: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                     original_length: int = 0, fast: float = 32.0, slow: float = 1.0) -> Tuple[torch.Tensor, float]:
+    """(radians per position fp64 [rot/2], magnitude of the rotation) of base^(-2i/rot), as they are
+    or scaled for contexts `factor` times longer than `original_length`:
+      "linear"    every frequency divided by factor (positions compressed)
+      "base"      the base raised by factor^(rot/(rot-2)): the fastest pair stays, the slowest is divided by factor
+      "by_parts"  pairs that turn more than `fast` times within original_length stay, those under `slow` turns are
+                  divided by factor, those between in proportion; magnitude 1 + 0.1 ln(factor)"""
+    i = torch.arange(0, rot, 2, dtype=torch.float64)
+    if scaling == "base":
+        _require(rot > 2, "a scaled base needs more than one pair")
+        base = base * factor ** (rot / (rot - 2))
+    f = base ** (-i / rot)
+    if scaling == "linear":
+        return f / factor, 1.0
+    if scaling == "by_parts":
+        _require(original_length > 0 and fast > slow, "by_parts needs original_length and fast > slow")
+        turns = f * original_length / (2 * math.pi)
+        keep = ((turns - slow) / (fast - slow)).clamp(0.0, 1.0)
+        return f * keep + f / factor * (1 - keep), 1.0 + 0.1 * math.log(factor) if factor > 1 else 1.0
+    _require(scaling in (None, "base"), f"unknown scaling {scaling!r}")
+    return f, 1.0
+
+
+def rope_table(length: int, inv_freq: torch.Tensor, magnitude: float = 1.0, device="cuda") -> torch.Tensor:
+    """cos and sin of m * inv_freq[i] for m < length, angles in fp64: fp32 [length, pairs, 2]."""
+    f = inv_freq.to(device=device, dtype=torch.float64).contiguous()
+    table = torch.empty((length, f.numel(), 2), dtype=torch.float32, device=f.device)
+    _check(LIB.fq_rope_table(_p(f), magnitude, length, f.numel(), _p(table), _stream()))
+    return table
+
+
+def qk_rope(q: torch.Tensor, k: Optional[torch.Tensor], table: Optional[torch.Tensor],
+            positions: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+            k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+            q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """Norms of queries and keys per head (where a weight fp32 [D] is given) and the rotation of their first
+    2 * table.shape[1] dims, halves or (interleaved) adjacent pairs: bf16 q [T, Hq, D], k [T, Hk, D], any strides of
+    multiples of 8 -> contiguous (q_out, k_out).  positions int32 [T] (None: 0, 1, ...)."""
+    T, Hq, D = q.shape
+    Hk = 0
+    if k is not None:
+        Hk = k.shape[1]
+        _require(tuple(k.shape) == (T, Hk, D), "k: [T, Hk, D] of q's T and D")
+    rope = _rope_desc(table, positions, T, q_weight, k_weight, D, eps, interleaved)
+    yq = _check_rows(q_out, q, "q_out")
+    yk = None if k is None else _check_rows(k_out, k, "k_out")
+    _check(LIB.fq_qk_rope(_heads(q, "q"), Hq, None if k is None else _heads(k, "k"), Hk, rope, T, D, yq.data_ptr(),
+                          _ptr(yk), _stream_handle()))
+    return yq, yk
+
+
+def cache_append(cache: KVCache, page_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, max_new: int,
+                 k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+                 table: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                 q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 interleaved: bool = False, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Appends the tokens of a ragged batch (rows q_start[b] .. q_start[b+1] - 1 of k, v [T, Hk, D] are the last ones of
+    the kv_len[b] tokens of sequence b) to its pages: keys normed and rotated as by qk_rope, keys and values rounded to 8
+    bits under a scale per page and head.  q [T, Hq, D] is normed and rotated in the same launch and returned.
+    max_new: the most rows of a sequence.  positions: None for a token's place in its sequence."""
+    T, H, D = k.shape
+    desc, ch, cd = _cache_desc(cache)
+    _require(H == ch and D == cd and tuple(v.shape) == (T, H, D), "k, v: [T, heads, D] of the cache's heads and D")
+    batch = _batch_desc(page_table, q_start, kv_len, max_new, page_tokens=cache.k_codes.shape[2])
+    y, Hq, hq = None, 0, None
+    if q is not None:
+        Hq = q.shape[1]
+        _require(tuple(q.shape) == (T, Hq, D), "q: [T, Hq, D] of k's T and D")
+        y, hq = _check_rows(q_out, q, "q_out"), _heads(q, "q")
+    rope = _rope_desc(table, positions, T, q_weight, k_weight, D, eps, interleaved)
+    _check(LIB.fq_cache_append(desc, batch, _heads(k, "k"), _heads(v, "v"), hq, Hq, rope, T, _ptr(y), _stream_handle()))
+    return y
+
+
+def cache_read(cache: KVCache, page_table: torch.Tensor, first: torch.Tensor, last: torch.Tensor, max_tokens: int,
+               k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Tokens first[b] .. last[b] - 1 of every sequence as values: bf16 k, v [seqs, max_tokens, heads, D], zeros beyond."""
+    desc, H, D = _cache_desc(cache)
+    _require(page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous(),
+             "page_table: contiguous int32 [seqs, pages]")
+    B, width = page_table.shape
+    shape = (B, max_tokens, H, D)
+    for o, name in ((k_out, "k_out"), (v_out, "v_out")):
+        _require(o is None or (o.dtype == torch.bfloat16 and tuple(o.shape) == shape and o.is_contiguous()),
+                 f"{name}: contiguous bf16 {shape}")
+    k = torch.empty(shape, dtype=torch.bfloat16, device=page_table.device) if k_out is None else k_out
+    v = torch.empty(shape, dtype=torch.bfloat16, device=page_table.device) if v_out is None else v_out
+    _check(LIB.fq_cache_read(desc, page_table.data_ptr(), width, _index(first, B, "first"), _index(last, B, "last"), B,
+                             max_tokens, k.data_ptr(), v.data_ptr(), _stream_handle()))
+    return k, v
+
+
+def cache_attention_workspace_bytes(T: int, Hq: int, Hk: int, D: int, seqs: int, max_new: int, max_kv: int) -> int:
+    return int(LIB.fq_cache_attention_workspace_bytes(T, Hq, Hk, D, seqs, max_new, max_kv))
+
+
+def cache_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
+                    max_new: int, max_kv: int, scale: Optional[float] = None, causal: bool = True,
+                    ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """softmax(scale q k^T) v of a ragged batch of queries bf16 [T, Hq, D] over its sequences' tokens in the cache (see
+    cache_append; append first) -> [T, Hq, D].  max_new, max_kv: the most rows and tokens of a sequence; scale: None for
+    1/sqrt(D); causal: a row sees the tokens up to its own place, otherwise all kv_len[b]."""
+    T, Hq, D = q.shape
+    desc, H, cd = _cache_desc(cache)
+    _require(D == cd, "q: [T, Hq, D] of the cache's D")
+    batch = _batch_desc(page_table, q_start, kv_len, max_new, max_kv)
+    y = _check_rows(out, q, "out")
+    if ws is None:
+        ws = _scratch(LIB.fq_cache_attention_workspace_bytes(T, Hq, H, D, page_table.shape[0], max_new, max_kv), q.device)
+    _check(LIB.fq_cache_attention(_heads(q, "q"), Hq, T, desc, batch, D ** -0.5 if scale is None else scale, int(causal),
+                                  y.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(), _stream_handle()))
+    return y
+
+
+def cross_attention_workspace_bytes(B: int, Sq: int, Sk: int, Hq: int, Hk: int, D: int) -> int:
+    return int(LIB.fq_cross_attention_workspace_bytes(B, Sq, Sk, Hq, Hk, D))
+
+
+def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kv_len: Optional[torch.Tensor] = None,
+                    key_mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                    ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """softmax(scale q k^T) v of queries bf16 [B, Sq, Hq, D] over an encoder's states k, v [B, Sk, Hk, D] (any strides of
+    multiples of 8) -> [B, Sq, Hq, D].  kv_len int32 [B]: states in use; key_mask bool [B, Sk]: True = seen.  What lies in
+    unseen places has no effect; a sample that sees nothing gives zeros."""
+    B, Sq, Hq, D = q.shape
+    Sk, Hk = k.shape[1], k.shape[2]
+    _require(tuple(k.shape) == (B, Sk, Hk, D) and v.shape == k.shape, "k, v: [B, Sk, Hk, D] of q's B and D")
+    stride = 0
+    if key_mask is not None:
+        _require(key_mask.dtype in (torch.bool, torch.uint8) and tuple(key_mask.shape) == (B, Sk)
+                 and (Sk < 2 or key_mask.stride(1) == 1), "key_mask: bool [B, Sk] with unit stride of the last dim")
+        stride = key_mask.stride(0)
+    y = _check_rows(out, q, "out")
+    if ws is None:
+        ws = _scratch(LIB.fq_cross_attention_workspace_bytes(B, Sq, Sk, Hq, Hk, D), q.device)
+    _check(LIB.fq_cross_attention(_heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _index(kv_len, B, "kv_len") or None,
+                                  _ptr(key_mask), stride, B, Sq, Sk, Hq, Hk, D, D ** -0.5 if scale is None else scale,
+                                  y.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(), _stream_handle()))
+    return y
