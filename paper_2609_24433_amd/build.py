@@ -23,7 +23,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libfq.so")
 SOURCES = ["fq_api.cpp", "fq_quant.hip", "fq_rotate.hip", "fq_gemm.hip", "fq_gemm_kg.hip", "fq_gemm_wide.hip", "fq_gptq.hip",
-           "fq_small.hip", "fq_attn_api.cpp", "fq_rope.hip", "fq_attn.hip"]
+           "fq_small.hip", "fq_attn_api.cpp", "fq_rope.hip", "fq_attn.hip", "fq_attn_tile.hip", "fq_attn_stream.hip"]
 ARCH = "gfx950"
 
 COMMON_FLAGS = [
@@ -33,7 +33,8 @@ COMMON_FLAGS = [
 ]
 
 
-EXTRA_FLAGS = {"fq_gemm.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "fq_small.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+_MFMA_VGPR = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+EXTRA_FLAGS = {name: _MFMA_VGPR for name in ("fq_gemm.hip", "fq_small.hip", "fq_attn_tile.hip", "fq_attn_stream.hip")}
 
 
 def _hipcc() -> str:

@@ -277,7 +277,7 @@ size_t fq_cache_attention_workspace_bytes(int64_t T, int Hq, int Hk, int D, int6
                                           int64_t max_kv) {
   if (T <= 0 || Hq < 1 || Hk < 1 || Hq % Hk || D < 16 || D > 256 || D % 16 || seqs <= 0 || max_new <= 0 || max_kv <= 0)
     return 0;
-  return attention_workspace(true, T, Hq, Hk, D, seqs, max_new, max_kv);
+  return attention_workspace(Hq, Hk, D, seqs, max_new, max_kv);
 }
 
 fq_status fq_cache_attention(const fq_heads *q, int Hq, int64_t T, const fq_kv_cache *cache, const fq_kv_batch *batch,
@@ -317,7 +317,7 @@ fq_status fq_cache_attention(const fq_heads *q, int Hq, int64_t T, const fq_kv_c
 
 size_t fq_cross_attention_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, int Hq, int Hk, int D) {
   if (B <= 0 || Sq <= 0 || Sk <= 0 || Hq < 1 || Hk < 1 || Hq % Hk || D < 16 || D > 256 || D % 16) return 0;
-  return attention_workspace(false, B * Sq, Hq, Hk, D, B, Sq, Sk);
+  return attention_workspace(Hq, Hk, D, B, Sq, Sk);
 }
 
 fq_status fq_cross_attention(const fq_heads *q, const fq_heads *k, const fq_heads *v, const int32_t *kv_len,

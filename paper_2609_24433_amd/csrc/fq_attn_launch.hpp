@@ -1,0 +1,15 @@
+// The attention kernels' launchers (fq_attn.hip chooses between them).
+#pragma once
+
+#include <atomic>
+
+#include "fq_attn_device.hpp"
+#include "fq_launch.hpp"
+
+namespace fq {
+
+int attention_tile_rows();
+hipError_t launch_attention_tile(bool cached, const AttnArgs &a, const Split &sp, hipStream_t s);
+hipError_t launch_attention_stream(bool cached, const AttnArgs &a, const Split &sp, hipStream_t s);
+
+}  // namespace fq
