@@ -9,90 +9,116 @@ namespace {
 constexpr int kStreamRows = 16;
 
 struct Plan {
-  bool stream;
-  int64_t chunk;
+  int rows;   // of a workgroup: 16 streaming, 128 or 256 with tiles
+  int chunk;  // tokens of a part
   int splits;
 };
 
-// Workgroups of both kernels hold four waves and two of them fit a compute unit, so 512 fill the
-// card.  Where the rows alone give fewer, or few rows leave ragged lengths to balance, the tokens
-// are split.
-Plan plan_attention(int Hq, int Hk, int64_t seqs, int64_t max_new, int64_t max_kv) {
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Streaming: parts of 256 tokens of a cache or 128 states (the same bytes at two a value), so that
+// waves of ragged sequences end evenly: 64 sequences of up to 8192 tokens take 82 us with parts of
+// 256, 94 with 512, 105 with 1024; parts under that pay their start-up (131 with 128 workgroups'
+// worth).  Parts get longer where there would be more than 32768 of them (their results cost room
+// and time) and shorter, down to a tile, where there are too few to fill the card: one sequence of
+// 877 tokens takes 13 us with 64, 19 with 128, 28 with 256.
+// Tiles: 256 rows a workgroup of eight waves where there are more than 128 rows and the head size
+// leaves the registers (head 128, 4096 rows over 8190 tokens: 414 us, with 128 rows 444), one a
+// compute unit; two of 128 rows fit otherwise.  Tokens are split only to fill the card, 128 or more
+// a part.
+Plan plan_attention(bool cached, int Hq, int Hk, int D, int64_t seqs, int64_t max_new, int64_t max_kv) {
   Plan p;
   const int64_t rows = max_new * (Hq / Hk);
-  p.stream = rows <= kStreamRows;
-  const int64_t per = p.stream ? 16 : attention_tile_rows();
-  const int64_t groups = seqs * Hk * ((rows + per - 1) / per);
-  const int64_t unit = p.stream ? 256 : 128;           // least tokens of a workgroup
-  const int64_t want = p.stream ? 2048 : 512;          // workgroups
-  int64_t splits = groups >= want ? 1 : want / groups;
-  const int64_t most = (max_kv + unit - 1) / unit;
-  if (splits > most) splits = most;
-  if (splits < 1) splits = 1;
-  p.chunk = ((max_kv + splits - 1) / splits + unit - 1) / unit * unit;
-  p.splits = p.chunk > 0 ? (int)((max_kv + p.chunk - 1) / p.chunk) : 1;
-  if (p.splits <= 1) {
-    p.splits = 1;
-    p.chunk = (int64_t)1 << 40;
+  const bool stream = rows <= kStreamRows;
+  p.rows = stream ? 16 : rows > 128 && D > 64 && D <= 128 ? 256 : 128;
+  const int64_t groups = seqs * Hk * ceil_div(rows, p.rows);
+  int64_t chunk;
+  if (stream) {
+    chunk = ceil_div(ceil_div(max_kv * groups, 32768), 64) * 64;
+    const int64_t least = cached ? 256 : 128;
+    if (chunk < least) chunk = least;
+    while (chunk > 64 && groups * ceil_div(max_kv, chunk) < 1024) chunk /= 2;
+    chunk = ceil_div(chunk, 64) * 64;
+  } else {
+    const int64_t want = p.rows == 256 ? 256 : 512, splits = groups >= want ? 1 : want / groups;
+    chunk = ceil_div(ceil_div(max_kv, splits), 128) * 128;
   }
+  p.splits = max_kv > chunk ? (int)ceil_div(max_kv, chunk) : 1;
+  p.chunk = p.splits > 1 ? (int)chunk : 1 << 30;
   return p;
 }
 
-// One row a wave: the weighted mean of its parts.
+// A row's result from its parts, 4 channels a lane: `lanes` lanes a part, `ways` parts of a row at
+// once (each way keeps its own maximum; they are joined in LDS).  A workgroup has 256 / (lanes ways)
+// units; a unit is a row, or with fewer lanes than channels / 4 a slice of its channels.
 template <bool CACHED>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, Split sp) {
-  const int lane = threadIdx.x % 64;
+__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, Split sp, int log_lanes, int log_ways, int slices) {
+  __shared__ float4 os[256];
+  __shared__ float2 mls[256];
   const int D = a.D, G = a.Hq / a.Hk;
+  const int way = (threadIdx.x >> log_lanes) & ((1 << log_ways) - 1);
   const int64_t s = blockIdx.y;
-  const int64_t per_seq = a.max_new * a.Hq;
-  const int64_t x = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-  if (x >= per_seq) return;
+  const int64_t unit = ((int64_t)blockIdx.x << (8 - log_lanes - log_ways)) + (threadIdx.x >> (log_lanes + log_ways));
+  const int64_t x = unit / slices;
+  const int c = (int)(unit - x * slices) << log_lanes | (threadIdx.x & ((1 << log_lanes) - 1));
   const Rows rows = sequence_queries<CACHED>(a, s);
   const int64_t i = x / a.Hq;
   const int hq = (int)(x - i * a.Hq), h = hq / G;
-  if (i >= rows.n) return;
-  const int64_t end = rows.end(i);
-  const int parts = end <= 0 ? 0 : (int)((end + sp.chunk - 1) / sp.chunk);
+  const bool row = i < rows.n;
+  const int end = row ? rows.end((int)i) : 0;
+  const int parts = (int)(((int64_t)end + sp.chunk - 1) / sp.chunk);
   const int64_t stride = a.seqs * a.Hk * a.max_new * G;
   const int64_t at = (s * a.Hk + h) * (a.max_new * G) + i * G + hq % G;
-  float m = -FLT_MAX;
-  for (int p = lane; p < parts; p += 64) m = maxf(m, sp.ml[p * stride + at].x);
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) m = maxf(m, __shfl_xor(m, d));
-  float o[4] = {0, 0, 0, 0}, l = 0.0f;
-  if (4 * lane < D)
-    for (int p = 0; p < parts; ++p) {
-      const float2 ml = sp.ml[p * stride + at];
-      const float w = exp2_fast(ml.x - m);
-      const float4 v = *reinterpret_cast<const float4 *>(sp.o + (p * stride + at) * D + 4 * lane);
-      l += ml.y * w;
-      o[0] += v.x * w, o[1] += v.y * w, o[2] += v.z * w, o[3] += v.w * w;
-    }
+  const bool in = 4 * c < D;
+  float m = -FLT_MAX, l = 0.0f;
+  float4 o = make_float4(0, 0, 0, 0);
+  auto join = [&](float2 ml, float4 v) {
+    const float to = maxf(m, ml.x), w0 = exp2_fast(m - to), w1 = exp2_fast(ml.x - to);
+    m = to;
+    l = l * w0 + ml.y * w1;
+    o = make_float4(o.x * w0 + v.x * w1, o.y * w0 + v.y * w1, o.z * w0 + v.z * w1, o.w * w0 + v.w * w1);
+  };
+#pragma unroll 4
+  for (int p = way; p < parts; p += 1 << log_ways)
+    join(sp.ml[p * stride + at], in ? *reinterpret_cast<const float4 *>(sp.o + (p * stride + at) * D + 4 * c) : make_float4(0, 0, 0, 0));
+  if (log_ways > 0) {
+    os[threadIdx.x] = o;
+    mls[threadIdx.x] = make_float2(m, l);
+    __syncthreads();
+    if (way > 0) return;
+    for (int w = 1; w < 1 << log_ways; ++w) join(mls[threadIdx.x + (w << log_lanes)], os[threadIdx.x + (w << log_lanes)]);
+  }
+  if (!row || !in) return;
   const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-  if (4 * lane < D)
-    *reinterpret_cast<uint2 *>(a.out + ((rows.q0 + i) * a.Hq + hq) * D + 4 * lane) =
-        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+  *reinterpret_cast<uint2 *>(a.out + ((rows.q0 + i) * a.Hq + hq) * D + 4 * c) =
+      make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
 }
 
 }  // namespace
 
-size_t attention_workspace(int Hq, int Hk, int D, int64_t seqs, int64_t max_new, int64_t max_kv) {
-  const Plan p = plan_attention(Hq, Hk, seqs, max_new, max_kv);
+size_t attention_workspace(bool cached, int Hq, int Hk, int D, int64_t seqs, int64_t max_new, int64_t max_kv) {
+  const Plan p = plan_attention(cached, Hq, Hk, D, seqs, max_new, max_kv);
   if (p.splits <= 1) return 0;
   return (size_t)p.splits * (size_t)seqs * (size_t)max_new * Hq * (D + 2) * 4;
 }
 
 hipError_t launch_attention(bool cached, const AttnArgs &a, void *ws, hipStream_t s) {
-  const Plan p = plan_attention(a.Hq, a.Hk, a.seqs, a.max_new, a.max_kv);
+  const Plan p = plan_attention(cached, a.Hq, a.Hk, a.D, a.seqs, a.max_new, a.max_kv);
   Split sp{p.chunk, p.splits, static_cast<float *>(ws), nullptr};
   if (p.splits > 1) sp.ml = reinterpret_cast<float2 *>(sp.o + (size_t)p.splits * a.seqs * a.max_new * a.Hq * a.D);
-  hipError_t e = p.stream ? launch_attention_stream(cached, a, sp, s) : launch_attention_tile(cached, a, sp, s);
+  hipError_t e = p.rows == 16 ? launch_attention_stream(cached, a, sp, s) : launch_attention_tile(cached, a, sp, p.rows, s);
   if (e != hipSuccess || p.splits <= 1) return e;
-  const dim3 grid((unsigned)((a.max_new * a.Hq + 3) / 4), (unsigned)a.seqs);
+  // channels over lanes, slices of 16 where whole rows would leave the card empty; then parts over ways
+  int log_lanes = 2, log_ways = 0, slices = 1;
+  while ((4 << log_lanes) < a.D) ++log_lanes;
+  while (log_lanes > 2 && p.splits > 32 && a.seqs * a.max_new * a.Hq * slices < 512) --log_lanes, slices *= 2;
+  while (log_lanes + log_ways < 8 && (4 << log_ways) < p.splits) ++log_ways;
+  const int per = 8 - log_lanes - log_ways;
+  const dim3 grid((unsigned)((a.max_new * a.Hq * slices + (1 << per) - 1) >> per), (unsigned)a.seqs);
   if (cached)
-    attention_join_kernel<true><<<grid, 256, 0, s>>>(a, sp);
+    attention_join_kernel<true><<<grid, 256, 0, s>>>(a, sp, log_lanes, log_ways, slices);
   else
-    attention_join_kernel<false><<<grid, 256, 0, s>>>(a, sp);
+    attention_join_kernel<false><<<grid, 256, 0, s>>>(a, sp, log_lanes, log_ways, slices);
   return hipGetLastError();
 }
 

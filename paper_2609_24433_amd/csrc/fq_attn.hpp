@@ -64,7 +64,7 @@ struct AttnArgs {
   const uint8_t *mask;
   int64_t mask_stride;
 };
-size_t attention_workspace(int Hq, int Hk, int D, int64_t seqs, int64_t max_new, int64_t max_kv);
+size_t attention_workspace(bool cached, int Hq, int Hk, int D, int64_t seqs, int64_t max_new, int64_t max_kv);
 hipError_t launch_attention(bool cached, const AttnArgs &a, void *ws, hipStream_t s);
 
 }  // namespace fq

@@ -47,7 +47,7 @@ fq_status check_heads(const char *what, const fq_heads *x, int64_t B, int64_t S,
   h.hs = H > 1 ? x->head_stride : 0;
   if (h.bs < 0 || h.ts < 0 || h.hs < 0) return fail(FQ_ERR_SHAPE, "%s: a stride is negative", what);
   if (h.bs % 8 || h.ts % 8 || h.hs % 8) return fail(FQ_ERR_ALIGN, "%s: strides must be multiples of 8", what);
-  if (h.bs > (1ll << 40) || h.ts > (1ll << 32) || h.hs > (1ll << 32))
+  if (h.bs > (1ll << 40) || h.ts > (1ll << 24) || h.hs > (1ll << 32))
     return fail(FQ_ERR_UNSUPPORTED, "%s: a stride is too large", what);
   *out = h;
   return FQ_OK;
@@ -277,7 +277,7 @@ size_t fq_cache_attention_workspace_bytes(int64_t T, int Hq, int Hk, int D, int6
                                           int64_t max_kv) {
   if (T <= 0 || Hq < 1 || Hk < 1 || Hq % Hk || D < 16 || D > 256 || D % 16 || seqs <= 0 || max_new <= 0 || max_kv <= 0)
     return 0;
-  return attention_workspace(Hq, Hk, D, seqs, max_new, max_kv);
+  return attention_workspace(true, Hq, Hk, D, seqs, max_new, max_kv);
 }
 
 fq_status fq_cache_attention(const fq_heads *q, int Hq, int64_t T, const fq_kv_cache *cache, const fq_kv_batch *batch,
@@ -317,7 +317,7 @@ fq_status fq_cache_attention(const fq_heads *q, int Hq, int64_t T, const fq_kv_c
 
 size_t fq_cross_attention_workspace_bytes(int64_t B, int64_t Sq, int64_t Sk, int Hq, int Hk, int D) {
   if (B <= 0 || Sq <= 0 || Sk <= 0 || Hq < 1 || Hk < 1 || Hq % Hk || D < 16 || D > 256 || D % 16) return 0;
-  return attention_workspace(Hq, Hk, D, B, Sq, Sk);
+  return attention_workspace(false, Hq, Hk, D, B, Sq, Sk);
 }
 
 fq_status fq_cross_attention(const fq_heads *q, const fq_heads *k, const fq_heads *v, const int32_t *kv_len,

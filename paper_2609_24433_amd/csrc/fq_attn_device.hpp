@@ -38,6 +38,16 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
+// Sum of two packed bf16 values and an fp32 one.
+__device__ __forceinline__ float add_pair(uint32_t pair, float sum) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), one, sum, false);
+#else
+  return sum;
+#endif
+}
+
 // Four int8 codes -> four bf16 (exact: |code| <= 128 has at most 8 significant bits): the float of
 // a code holds it in its upper half.
 __device__ __forceinline__ uint2 codes_to_bf16(uint32_t w) {
@@ -88,40 +98,43 @@ __device__ __forceinline__ uint2 lds_read_transposed(const void *p) {
 #endif
 }
 
-// The rows of one sequence: row r of a key head is query i = r / G, head h G + r % G.
+// The rows of one sequence: row r of a key head is query i = r / G, head h G + r % G.  Counts and
+// places of tokens are below 2^30, rows of a key head below 2^31.
 struct Rows {
-  int64_t q0;    // first row of the sequence in q and out
-  int64_t n;     // queries
-  int64_t keys;  // keys there are
-  int64_t back;  // causal: query i sees keys up to back + i
+  int64_t q0;   // first row of the sequence in q and out
+  int n;        // queries
+  int keys;     // keys there are
+  int back;     // causal: query i sees keys up to back + i
   bool causal;
   // keys that query i sees: [0, end(i))
-  __device__ __forceinline__ int64_t end(int64_t i) const {
+  __device__ __forceinline__ int end(int i) const {
     if (!causal) return keys;
-    const int64_t e = back + i + 1;
+    const int e = back + i + 1;
     return e < 0 ? 0 : e < keys ? e : keys;
   }
 };
 template <bool CACHED>
 __device__ __forceinline__ Rows sequence_queries(const AttnArgs &a, int64_t s) {
   Rows r;
+  const int max_new = (int)a.max_new, max_kv = (int)a.max_kv;
   if constexpr (CACHED) {
-    int64_t q0 = a.b.q_start[s], q1 = a.b.q_start[s + 1];
-    q0 = q0 < 0 ? 0 : q0 > a.T ? a.T : q0;
-    q1 = q1 < q0 ? q0 : q1 > a.T ? a.T : q1;
-    const int64_t len = a.b.kv_len[s];
+    const int T = (int)a.T;
+    int q0 = a.b.q_start[s], q1 = a.b.q_start[s + 1];
+    q0 = q0 < 0 ? 0 : q0 > T ? T : q0;
+    q1 = q1 < q0 ? q0 : q1 > T ? T : q1;
+    const int len = a.b.kv_len[s] < 0 ? 0 : a.b.kv_len[s];
     r.q0 = q0;
-    r.n = q1 - q0 < a.max_new ? q1 - q0 : a.max_new;
-    r.keys = len < a.max_kv ? (len < 0 ? 0 : len) : a.max_kv;
+    r.n = q1 - q0 < max_new ? q1 - q0 : max_new;
+    r.keys = len < max_kv ? len : max_kv;
     r.back = len - (q1 - q0);
     r.causal = a.causal != 0;
   } else {
     r.q0 = s * a.max_new;
-    r.n = a.max_new;
-    r.keys = a.max_kv;
+    r.n = max_new;
+    r.keys = max_kv;
     if (a.kv_len) {
-      const int64_t len = a.kv_len[s];
-      r.keys = len < 0 ? 0 : len < r.keys ? len : r.keys;
+      const int len = a.kv_len[s];
+      r.keys = len < 0 ? 0 : len < max_kv ? len : max_kv;
     }
     r.back = 0;
     r.causal = false;
@@ -129,16 +142,18 @@ __device__ __forceinline__ Rows sequence_queries(const AttnArgs &a, int64_t s) {
   return r;
 }
 
+__device__ __forceinline__ int clamp_page(int p, int64_t pages) {
+  return p < 0 ? 0 : p >= pages ? (int)(pages - 1) : p;
+}
 __device__ __forceinline__ int64_t cache_page(const AttnArgs &a, int64_t s, int64_t w) {
-  const int64_t p = a.b.pt[s * a.b.width + w];
-  return p < 0 ? 0 : p >= a.c.pages ? a.c.pages - 1 : p;
+  return clamp_page(a.b.pt[s * a.b.width + w], a.c.pages);
 }
 
 // How a call's tokens are split: `splits` ranges of `chunk` tokens; with more than one, fp32
 // partial results o [splits][seqs][Hk][max_new G][D] and (maximum, sum) ml [splits][...] go to the
 // workspace and a second kernel joins them.
 struct Split {
-  int64_t chunk;
+  int chunk;
   int splits;
   float *o;
   float2 *ml;

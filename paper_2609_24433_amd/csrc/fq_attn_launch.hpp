@@ -8,8 +8,8 @@
 
 namespace fq {
 
-int attention_tile_rows();
-hipError_t launch_attention_tile(bool cached, const AttnArgs &a, const Split &sp, hipStream_t s);
+// rows: of a workgroup, 128 or (head sizes up to 128) 256
+hipError_t launch_attention_tile(bool cached, const AttnArgs &a, const Split &sp, int rows, hipStream_t s);
 hipError_t launch_attention_stream(bool cached, const AttnArgs &a, const Split &sp, hipStream_t s);
 
 }  // namespace fq

@@ -1,13 +1,12 @@
 // Attention for few query rows: up to 16 rows of one key head, where the keys and values are read
-// once from memory.  The four waves of a workgroup take its tokens in turn, each a tile at a time
-// straight from memory into the operands of the matrix instruction, and join their results.
+// once from memory.  A workgroup is one wave that walks its part of the tokens, a tile at a time
+// straight from memory into the operands of the matrix instruction: waves share nothing, so a
+// wave that ends makes room for the next at once, whatever the sequences' lengths.
 #include "fq_attn_device.hpp"
 #include "fq_attn_launch.hpp"
 
 namespace fq {
 namespace {
-
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
 // Tokens a wave takes at once.  A lane (row l % 16, group g = l / 16 of the operands' k) holds the
 // scores of NT / 4 consecutive tokens, 16 g .. of 64 or 8 g .. of 32: cached tiles have 64, one
@@ -18,24 +17,14 @@ struct Tile {
   static constexpr int kBlocks = kTokens / 16;  // 16-token products
 };
 
-// The waves' results: maximum, sum and O^T of the same 16 rows, two waves at a time.
-template <int DP>
-struct Joined {
-  float o[2][DP / 4][64];
-  float m[2][64], l[2][64];
-};
-
 template <bool CACHED, int DP>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_stream_kernel(AttnArgs a, Split sp, int row_tiles) {
+__global__ __launch_bounds__(64, DP == 256 ? 2 : 3) void attention_stream_kernel(AttnArgs a, Split sp, int row_tiles) {
   constexpr int NT = Tile<CACHED>::kTokens, NB = Tile<CACHED>::kBlocks, PER = NT / 4;
   constexpr int C = DP / 64;  // 64-channel steps: a lane group reads 16 channels of each
   constexpr int DT = DP / 16;
   constexpr int kVStride = 2 * DP + 32;  // values of the wave's tile in LDS (states): bytes of a token
-  __shared__ __align__(16) union {
-    Joined<DP> join;
-    uint8_t values[CACHED ? 16 : kWaves * 32 * kVStride];
-  } lds;
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  __shared__ __align__(16) uint8_t mine[CACHED ? 16 : 32 * kVStride];
+  const int lane = threadIdx.x;
   const int col = lane % 16, g = lane / 16;
   const int D = a.D, G = a.Hq / a.Hk;
   const int h = blockIdx.x % a.Hk;
@@ -43,19 +32,19 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_stream_
   const int part = blockIdx.x / a.Hk / row_tiles;
   const int64_t s = blockIdx.y;
   const Rows rows = sequence_queries<CACHED>(a, s);
-  const int64_t total = rows.n * G, r0 = (int64_t)tile_row * 16;
+  const int total = rows.n * G, r0 = tile_row * 16;
   if (r0 >= total) return;
-  const int64_t last_row = r0 + 16 < total ? r0 + 15 : total - 1;
-  const int64_t c0 = (int64_t)part * sp.chunk;
-  const int64_t end_max = rows.end(last_row / G), end_min = rows.end(r0 / G);
-  const int64_t c1 = end_max < c0 + sp.chunk ? end_max : c0 + sp.chunk;
+  const int last_row = total - r0 > 16 ? r0 + 15 : total - 1;
+  const int c0 = part * sp.chunk;
+  const int end_max = rows.end(last_row / G), end_min = rows.end(r0 / G);
+  const int c1 = end_max - c0 > sp.chunk ? c0 + sp.chunk : end_max;
   if (c1 <= c0 && part > 0) return;  // no row of it has a partial result here
 
-  const int64_t r = r0 + col;
+  const int r = r0 + col;
   const bool live = r < total;
-  const int64_t qi = live ? r / G : 0;
-  const int hq = h * G + (int)(live ? r - qi * G : 0);
-  const int64_t end = live ? rows.end(qi) : 0;
+  const int qi = live ? r / G : 0;
+  const int hq = h * G + (live ? r - qi * G : 0);
+  const int end = live ? rows.end(qi) : 0;
 
   // channel order of the first product: step (c, e) has channels 64 c + 16 g + 8 e ..
   bf16x8 q[C][2];
@@ -85,19 +74,19 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_stream_
   float ks = 0.0f, vs = 0.0f;
   uint32_t bits = ~0u;
 
-  auto find = [&](int64_t j0) {
+  auto find = [&](int j0) {
     if constexpr (CACHED) {
-      const int64_t jk = j0 + 16 * (col / 4), jv = j0 + 16 * g;
+      const int jk = j0 + 16 * (col / 4), jv = j0 + 16 * g;
       page_k = jk < rows.keys ? cache_page(a, s, jk >> lp) * a.c.H + h : -1;
       page_v = jv < rows.keys ? cache_page(a, s, jv >> lp) * a.c.H + h : -1;
     } else {
-      const int64_t j = j0 + lane % 32;
+      const int j = j0 + lane % 32;
       bool on = j < rows.keys;
       if (on && a.mask) on = a.mask[s * a.mask_stride + j] != 0;
       bits = (uint32_t)__ballot(on);
     }
   };
-  auto fetch_keys = [&](int64_t j0) {
+  auto fetch_keys = [&](int j0) {
     if constexpr (CACHED) {
       ks = page_v >= 0 ? a.c.ks[page_v] : 0.0f;
       vs = page_v >= 0 ? a.c.vs[page_v] : 0.0f;
@@ -111,7 +100,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_stream_
             kr[t][c][0] = *reinterpret_cast<const uint4 *>(base + 4 * t * D + 64 * c + 16 * g);
         }
     } else {
-      const uint16_t *base = a.k.p + s * a.k.bs + h * a.k.hs + (j0 + krow) * a.k.ts + 16 * g;
+      const uint16_t *base = a.k.p + s * a.k.bs + h * a.k.hs + (int64_t)(j0 + krow) * a.k.ts + 16 * g;
 #pragma unroll
       for (int t = 0; t < NB; ++t) {
         const bool on = bits >> (krow + 4 * t) & 1;
@@ -126,7 +115,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_stream_
       }
     }
   };
-  auto fetch_values = [&](int64_t j0) {
+  auto fetch_values = [&](int j0) {
     if constexpr (CACHED) {
       const int8_t *base = a.c.vc + page_v * a.c.P * D + (int64_t)((j0 + 16 * g) & (a.c.P - 1)) * D + col * 16;
 #pragma unroll
@@ -140,20 +129,19 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_stream_
         const int u = lane + 64 * i, token = u / (DP / 8), piece = u % (DP / 8);
         vr[i] = make_uint4(0, 0, 0, 0);
         if ((bits >> token & 1) && 8 * piece < D)
-          vr[i] = *reinterpret_cast<const uint4 *>(a.v.p + s * a.v.bs + h * a.v.hs + (j0 + token) * a.v.ts + 8 * piece);
+          vr[i] = *reinterpret_cast<const uint4 *>(a.v.p + s * a.v.bs + h * a.v.hs + (int64_t)(j0 + token) * a.v.ts + 8 * piece);
       }
     }
   };
 
-  uint8_t *mine = lds.values + (CACHED ? 0 : wave * 32 * kVStride);
-  int64_t j0 = c0 + (int64_t)wave * NT;
+  int j0 = c0;
   if (j0 < c1) {
     find(j0);
     fetch_keys(j0);
     fetch_values(j0);
   }
-  for (; j0 < c1; j0 += kWaves * NT) {
-    const int64_t next = j0 + kWaves * NT;
+  for (; j0 < c1; j0 += NT) {
+    const int next = j0 + NT;
     const uint32_t bits_now = bits;
     const float ks_now = ks, vs_now = vs;
     f32x4 st[NB];
@@ -188,7 +176,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_stream_
     const bool masked = j0 + NT > end_min || (!CACHED && bits_now != ~0u);
     uint32_t on = (1u << PER) - 1;
     if (masked) {
-      const int64_t left = end - (j0 + PER * g);
+      const int left = end - (j0 + PER * g);
       on = left >= PER ? on : left <= 0 ? 0u : (1u << left) - 1;
       if (!CACHED) on &= bits_now >> (PER * g);
     }
@@ -238,35 +226,10 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_stream_
     if (next < c1) fetch_values(next);
   }
   l = across16(across32(l, [](float x, float y) { return x + y; }), [](float x, float y) { return x + y; });
-
-  // join the waves' results: 2 and 3 into 0 and 1, then 1 into 0
-#pragma unroll
-  for (int step = 2; step >= 1; step /= 2) {
-    __syncthreads();
-    if (wave >= step && wave < 2 * step) {
-#pragma unroll
-      for (int i = 0; i < DT; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) lds.join.o[wave - step][4 * i + e][lane] = o[i][e];
-      lds.join.m[wave - step][lane] = m;
-      lds.join.l[wave - step][lane] = l;
-    }
-    __syncthreads();
-    if (wave < step) {
-      const float om = lds.join.m[wave][lane], ol = lds.join.l[wave][lane];
-      const float to = maxf(m, om), x = exp2_fast(m - to), y = exp2_fast(om - to);
-      m = to;
-      l = l * x + ol * y;
-#pragma unroll
-      for (int i = 0; i < DT; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][e] = o[i][e] * x + lds.join.o[wave][4 * i + e][lane] * y;
-    }
-  }
-  if (wave > 0 || !live) return;
+  if (!live) return;
   // a lane holds channels 16 i + 4 g .. of its row
   if (sp.splits > 1) {
-    const int64_t at = ((part * a.seqs + s) * a.Hk + h) * (a.max_new * G) + r;
+    const int64_t at = (((int64_t)part * a.seqs + s) * a.Hk + h) * (a.max_new * G) + r;
     if (g == 0) sp.ml[at] = make_float2(m, l);
 #pragma unroll
     for (int i = 0; i < DT; ++i)
@@ -286,7 +249,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_stream_
 template <bool CACHED, int DP>
 hipError_t launch(const AttnArgs &a, const Split &sp, hipStream_t s) {
   const int64_t row_tiles = (a.max_new * (a.Hq / a.Hk) + 15) / 16;
-  attention_stream_kernel<CACHED, DP><<<dim3((unsigned)(a.Hk * row_tiles * sp.splits), (unsigned)a.seqs), kThreads, 0, s>>>(
+  attention_stream_kernel<CACHED, DP><<<dim3((unsigned)(a.Hk * row_tiles * sp.splits), (unsigned)a.seqs), 64, 0, s>>>(
       a, sp, (int)row_tiles);
   return hipGetLastError();
 }

@@ -1,29 +1,43 @@
-// Attention for many query rows: a workgroup of four waves holds 128 rows of one key head (32 a
-// wave) and walks the keys in tiles of 64 that all four waves read from LDS.
+// Attention for many query rows: a workgroup of four or eight waves holds 128 or 256 rows of one
+// key head (32 a wave) and walks the keys in tiles of 64 that all its waves read from LDS.
+//
+// A tile costs a wave about as many cycles of the vector unit (exponentials, conversion of codes) as
+// of the matrix unit, and a wave's vector instructions run while a matrix instruction of its own
+// does.  So the loop is a pipeline over half tiles u of 32 keys, written as two chains of matrix
+// instructions with a piece of vector work after each:
+//   K Q^T of u + 1     with  the weights (exponentials) of u
+//   V^T P^T of u       with  the last weights of u, the maxima of u + 1 and the staging of a tile's
+//                            values (first half: of the next tile) or keys (second: the one after)
+// Loads run a tile ahead of the staging.
 #include "fq_attn_device.hpp"
 #include "fq_attn_launch.hpp"
 
 namespace fq {
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves, kTile = 64;
+constexpr int kTile = 64;
 
 // LDS of a tile: keys [64][DP] bf16, the 16-byte pieces of a token's row swizzled; values
-// transposed [DP][64 + 8] (cache) or [64][DP + 16] (states, read with the transposing read).
+// transposed [DP][64 + 8] (cache) or [64][DP + 32] (states, read with the transposing read).  16
+// lanes of a 16-byte access, and 32 of an 8-byte one, meet all 64 banks once.
 template <bool CACHED, int DP>
 struct Lds {
   static constexpr int kKeys = kTile * DP * 2;
-  static constexpr int kVStride = CACHED ? 2 * kTile + 16 : 2 * DP + 32;  // bytes of a row
+  static constexpr int kVStride = CACHED ? 2 * kTile + 16 : 2 * DP + 64;  // bytes of a row
   static constexpr int kValues = (CACHED ? DP : kTile) * kVStride;
-  static constexpr int kBuffer = kKeys + kValues;
+  static constexpr int kBytes = 2 * (kKeys + kValues) + (CACHED ? 0 : 4 * kTile * 4);
 };
-// Eight lanes that read one piece of tokens 0-3 and 16-19 (+ 4 a) meet eight bank groups.
-__device__ __forceinline__ int swizzle(int token) { return (token & 3) | ((token >> 2) & 4); }
+// 16 lanes read one piece of tokens 0-7 and 16-23 (or 8-15 and 24-31).
+template <int DP>
+__device__ __forceinline__ int swizzle(int token) {
+  return DP == 64 ? ((token >> 1) & 3) | ((token >> 2) & 4) : (token & 7) | ((token >> 1) & 8);
+}
 
-template <bool CACHED, int DP>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_tile_kernel(AttnArgs a, Split sp, int row_tiles) {
+template <bool CACHED, int DP, int RT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_kernel(AttnArgs a, Split sp, int row_tiles) {
   extern __shared__ __align__(16) uint8_t lds[];
   using L = Lds<CACHED, DP>;
+  constexpr int kThreads = 64 * WAVES, kRows = 32 * RT * WAVES;
   constexpr int KU = kTile * (DP / 16) / kThreads;  // 16-channel pieces of keys a thread stages
   constexpr int VU = CACHED ? 4 * DP / kThreads : kTile * (DP / 8) / kThreads;
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -34,292 +48,512 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_tile_ke
   const int tile_row = row_tiles - 1 - blockIdx.x / a.Hk / sp.splits;  // longest rows first
   const int64_t s = blockIdx.y;
   const Rows rows = sequence_queries<CACHED>(a, s);
-  const int64_t total = rows.n * G, r0 = (int64_t)tile_row * kRows;
+  const int total = rows.n * G, r0 = tile_row * kRows;
   if (r0 >= total) return;
 
   // keys of the workgroup: its range, up to what its last row sees
-  const int64_t last_row = r0 + kRows < total ? r0 + kRows - 1 : total - 1;
-  const int64_t c0 = (int64_t)part * sp.chunk;
-  int64_t c1 = rows.end(last_row / G);
-  if (c1 > c0 + sp.chunk) c1 = c0 + sp.chunk;
+  const int last_row = total - r0 > kRows ? r0 + kRows - 1 : total - 1;
+  const int c0 = part * sp.chunk;
+  int c1 = rows.end(last_row / G);
+  if (c1 - c0 > sp.chunk) c1 = c0 + sp.chunk;
   if (c1 <= c0 && part > 0) return;  // no row of it has a partial result here
-  const int tiles = c1 > c0 ? (int)((c1 - c0 + kTile - 1) / kTile) : 0;
+  const int tiles = c1 > c0 ? (c1 - c0 + kTile - 1) / kTile : 0;
 
-  // this lane's row, as the column of both products
-  const int64_t r = r0 + wave * 32 + col;
-  const bool live = r < total;
-  const int64_t qi = live ? r / G : 0;
-  const int hq = h * G + (int)(live ? r - qi * G : 0);
-  const int64_t end = live ? rows.end(qi) : 0;
-  bf16x8 q[DP / 16];
-  {
-    const uint16_t *p = CACHED ? a.q.p + (rows.q0 + qi) * a.q.ts + hq * a.q.hs : a.q.p + s * a.q.bs + qi * a.q.ts + hq * a.q.hs;
+  // this lane's rows, one of each block, as the column of both products
+  bool live[RT];
+  int qi[RT], hq[RT], end[RT], end_min[RT];  // end_min: least that a row of the block sees
+  bf16x8 q[RT][DP / 16];
+#pragma unroll
+  for (int x = 0; x < RT; ++x) {
+    const int b0 = r0 + (wave * RT + x) * 32, r = b0 + col;
+    live[x] = r < total;
+    qi[x] = live[x] ? r / G : 0;
+    hq[x] = h * G + (live[x] ? r - qi[x] * G : 0);
+    end[x] = live[x] ? rows.end(qi[x]) : 0;
+    end_min[x] = b0 < total ? rows.end(b0 / G) : 0;
+    const uint16_t *p = CACHED ? a.q.p + (rows.q0 + qi[x]) * a.q.ts + hq[x] * a.q.hs
+                               : a.q.p + s * a.q.bs + qi[x] * a.q.ts + hq[x] * a.q.hs;
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) {
       uint4 u = make_uint4(0, 0, 0, 0);
-      if (live && 16 * i < D) u = *reinterpret_cast<const uint4 *>(p + 16 * i + 8 * half);
-      q[i] = __builtin_bit_cast(bf16x8, u);
+      if (live[x] && 16 * i < D) u = *reinterpret_cast<const uint4 *>(p + 16 * i + 8 * half);
+      q[x][i] = __builtin_bit_cast(bf16x8, u);
     }
   }
-  // least and most that a row of the wave sees, for the masks
-  const int64_t wr0 = r0 + wave * 32, wr1 = wr0 + 31 < total ? wr0 + 31 : total - 1;
-  const int64_t end_min = wr0 < total ? rows.end(wr0 / G) : 0, end_max = wr0 < total ? rows.end(wr1 / G) : 0;
 
-  f32x16 o[DP / 32];
+  f32x16 o[RT][DP / 32];
+  float m[RT], l[RT][2];  // l: of even and odd tokens
 #pragma unroll
-  for (int i = 0; i < DP / 32; ++i) o[i] = f32x16{};
-  float m = -FLT_MAX, l = 0.0f;
+  for (int x = 0; x < RT; ++x) {
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) o[x][i] = f32x16{};
+    m[x] = -FLT_MAX;
+    l[x][0] = l[x][1] = 0.0f;
+  }
   const float c_all = a.scale * 1.4426950408889634f;
 
-  // staging registers of the next tile
-  uint4 kr[CACHED ? KU : 2 * KU], vr[VU];
-  float ks[2], vs[2];
-  uint64_t seen_bits = ~0ull;
-
-  auto fetch = [&](int t) {
-    const int64_t j0 = c0 + (int64_t)t * kTile;
+  // Loads of the tiles to come.  Every load is unconditional, at an address that is there (channels
+  // from D on and tokens past the last one repeat others): what such places hold is finite or
+  // replaced, meets zeros of q or weights of zero, or goes to channels nobody reads.
+  struct Loaded {
+    uint4 k[CACHED ? KU : VU], v[VU];
+    float ks, vs;  // scales of 16-token group lane % 4
+    uint32_t mask;
+  };
+  Loaded in, hold;  // in flight; of the tiles to stage
+  const int last_key = rows.keys - 1;
+  // A cache's tile is four 16-token groups, each in a page of its own perhaps: lane % 4 finds its
+  // group's page, offset and scales, and a load takes its group's offset from that lane (the group
+  // of a unit is the same for a whole wave, and so is the unit's place in it for all units).
+  const int lp = CACHED ? 31 - __builtin_clz(a.c.P) : 0;
+  const int32_t *pt = CACHED ? a.b.pt + s * a.b.width : nullptr;
+  const int page_limit = CACHED ? (int)(a.c.pages - 1) : 0;
+  const uint32_t head_bytes = CACHED ? a.c.P * D : 0, in_page = a.c.P - 1;
+  const int8_t *kc = a.c.kc, *vc = a.c.vc;
+  const uint32_t key_place = (tid / (DP / 16) % 16) * D + 16 * (16 * (tid % (DP / 16)) < D ? tid % (DP / 16) : 0);
+  const uint32_t value_place = 16 * (tid % DP < D ? tid % DP : 0);
+  int page_next = 0;                  // looked up a tile ahead
+  int64_t at_k = 0, at_v = 0;         // byte offset of the group in the codes
+  int64_t scale_k = 0, scale_v = 0;   // index of its scales
+  auto look_up = [&](int t) {
+    const int j = c0 + t * kTile + 16 * (lane & 3);
+    page_next = pt[(j < last_key ? j : last_key) >> lp];
+  };
+  auto find = [&](int t) {
+    const int page = page_next < 0 ? 0 : page_next > page_limit ? page_limit : page_next;
+    scale_k = (int64_t)page * a.c.H + h;
+    at_k = scale_k * head_bytes + (uint32_t)(((c0 + t * kTile + 16 * (lane & 3)) & in_page) * D);
+  };
+  auto group_at = [&](int64_t at, int g) {
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)at, g), hi = __builtin_amdgcn_readlane((uint32_t)(at >> 32), g);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+  };
+  // States: a thread's places in a tile (bytes; the last tile's stop at the last state).
+  const uint16_t *kp = a.k.p + s * a.k.bs + h * a.k.hs, *vp = a.v.p + s * a.v.bs + h * a.v.hs;
+  uint32_t off_k[CACHED ? 1 : VU], off_v[CACHED ? 1 : VU];
+  auto places = [&](int last, int64_t ts, uint32_t(&off)[CACHED ? 1 : VU]) {
+    if constexpr (!CACHED)
+#pragma unroll
+      for (int i = 0; i < VU; ++i) {
+        const int u = tid + i * kThreads, tk = u / (DP / 8), piece = 8 * (u % (DP / 8));
+        off[i] = 2 * ((uint32_t)(tk < last ? tk : last) * (uint32_t)ts + (piece < D ? piece : 0));
+      }
+  };
+  places(kTile - 1, a.k.ts, off_k);
+  places(kTile - 1, a.v.ts, off_v);
+  auto load_keys = [&](int t) {
     if constexpr (CACHED) {
-      const int64_t hb = (int64_t)h;
-      const int lp = 31 - __builtin_clz(a.c.P);
-      // the 16-token group of a unit is the same for a whole wave
-      auto group_page = [&](int g) -> int64_t {
-        const int64_t j = j0 + 16 * g;
-        return j < rows.keys ? cache_page(a, s, j >> lp) * a.c.H + hb : -1;
+      find(t);
+#pragma unroll
+      for (int i = 0; i < KU; ++i) {
+        const int g = __builtin_amdgcn_readfirstlane((tid + i * kThreads) / DP);
+        in.k[i] = *reinterpret_cast<const uint4 *>(kc + group_at(at_k, g) + key_place);
+      }
+      in.ks = a.c.ks[scale_k];
+    } else {
+      const int j0 = c0 + t * kTile, last = last_key - j0;
+      if (last < kTile - 1) places(last < 0 ? 0 : last, a.k.ts, off_k);
+      const char *base = reinterpret_cast<const char *>(kp + (int64_t)(last < 0 ? last_key : j0) * a.k.ts);
+#pragma unroll
+      for (int i = 0; i < VU; ++i) in.k[i] = *reinterpret_cast<const uint4 *>(base + off_k[i]);
+    }
+  };
+  auto load_values = [&](int t) {
+    if constexpr (CACHED) {
+#pragma unroll
+      for (int i = 0; i < VU; ++i) {
+        const int g = __builtin_amdgcn_readfirstlane((tid + i * kThreads) / DP);
+        in.v[i] = *reinterpret_cast<const uint4 *>(vc + group_at(at_v, g) + value_place);
+      }
+      in.vs = a.c.vs[scale_v];
+    } else {
+      const int j0 = c0 + t * kTile, last = last_key - j0;
+      if (last < kTile - 1) places(last < 0 ? 0 : last, a.v.ts, off_v);
+      const char *base = reinterpret_cast<const char *>(vp + (int64_t)(last < 0 ? last_key : j0) * a.v.ts);
+#pragma unroll
+      for (int i = 0; i < VU; ++i) in.v[i] = *reinterpret_cast<const uint4 *>(base + off_v[i]);
+    }
+  };
+  // One place of a tile a lane: whether its state is seen.
+  auto load_mask = [&](int t) {
+    if constexpr (!CACHED) {
+      const int j = c0 + t * kTile + lane;
+      in.mask = j <= last_key;
+      if (a.mask) in.mask &= a.mask[s * a.mask_stride + (j <= last_key ? j : last_key)] != 0;
+    }
+  };
+  // Tile t's loads: its values, and the keys and the mask of the tile after it.
+  auto load = [&](int t) {
+    load_values(t);
+    load_keys(t + 1);
+    load_mask(t + 1);
+    at_v = at_k;
+    scale_v = scale_k;
+    if constexpr (CACHED) look_up(t + 2);
+  };
+
+  uint8_t *const keys_at = lds, *const values_at = lds + 2 * L::kKeys;
+  // Staging in pieces, 8 channels (tokens) of a unit each: the held keys go to buffer kb, the values
+  // to buffer vb.
+  constexpr int kKeyPieces = CACHED ? 2 * KU : VU, kValuePieces = CACHED ? 2 * VU : VU;
+  using KeyPieces = std::integral_constant<int, kKeyPieces>;
+  using ValuePieces = std::integral_constant<int, kValuePieces>;
+  auto stage_key = [&](uint8_t *to, int n) {
+    if constexpr (CACHED) {
+      const int i = n / 2, e = n % 2;
+      const int u = tid + i * kThreads, tk = u / (DP / 16), piece = 2 * (u % (DP / 16)) + e;
+      *reinterpret_cast<uint4 *>(to + tk * DP * 2 + ((piece ^ swizzle<DP>(tk)) * 16)) =
+          e == 0 ? codes8_to_bf16(hold.k[i].x, hold.k[i].y) : codes8_to_bf16(hold.k[i].z, hold.k[i].w);
+    } else {
+      const int u = tid + n * kThreads, tk = u / (DP / 8), piece = u % (DP / 8);
+      *reinterpret_cast<uint4 *>(to + tk * DP * 2 + ((piece ^ swizzle<DP>(tk)) * 16)) = hold.k[n];
+    }
+  };
+  auto stage_value = [&](uint8_t *to, int n) {
+    if constexpr (CACHED) {
+      const int j = n / 2, e = n % 2;
+      const int u = tid + j * kThreads, d = u % DP, g = u / DP;
+      *reinterpret_cast<uint4 *>(to + d * L::kVStride + g * 32 + 16 * e) =
+          e == 0 ? codes8_to_bf16(hold.v[j].x, hold.v[j].y) : codes8_to_bf16(hold.v[j].z, hold.v[j].w);
+    } else {
+      const int u = tid + n * kThreads, tk = u / (DP / 8), piece = u % (DP / 8);
+      *reinterpret_cast<uint4 *>(to + tk * L::kVStride + piece * 16) = hold.v[n];
+    }
+  };
+  // Unseen states: zeros for their keys and values (they may hold anything), zeros for channels from
+  // D on, and minus infinity where a tile's scores start from (one of four buffers).
+  float *const bias = reinterpret_cast<float *>(lds + 2 * (L::kKeys + L::kValues));
+  auto clear_rows = [&](uint4(&x)[VU], uint64_t seen) {
+    if (!CACHED && (D < DP || seen != ~0ull))
+#pragma unroll
+      for (int i = 0; i < VU; ++i) {
+        const int u = tid + i * kThreads, tk = u / (DP / 8), piece = 8 * (u % (DP / 8));
+        if (piece >= D || !(seen >> tk & 1)) x[i] = make_uint4(0, 0, 0, 0);
+      }
+  };
+  auto write_bias = [&](int t) {
+    if (!CACHED && wave == 0) bias[(t & 3) * kTile + lane] = hold.mask ? 0.0f : -INFINITY;
+  };
+
+  // S^T: row i = 8 x + 4 y + z of a 32-token block is token 16 y + 4 x + z
+  const int token = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3), sw = swizzle<DP>(token);
+  constexpr int STEPS = DP / 16;  // operands of a half tile, of either product
+  constexpr int AHEAD = 3;        // operands read ahead of the instructions that use them
+  // Keys' operand n of half b: channels 16 n ..; values' operand n: channels 32 (n % (DP/32)) .., step
+  // n / (DP/32) of 16 tokens, where a lane's are 32 b + 16 half + 8 step ..
+  auto key_operand = [&](const uint8_t *kb, int b, int n) {
+    return *reinterpret_cast<const uint4 *>(kb + (32 * b + token) * DP * 2 + (((2 * n + half) ^ sw) * 16));
+  };
+  auto value_operand = [&](const uint8_t *vb, int b, int n) {
+    const int i = n % (DP / 32), x = n / (DP / 32);
+    if constexpr (CACHED) {
+      return *reinterpret_cast<const uint4 *>(vb + (32 * i + col) * L::kVStride + (32 * b + 16 * half + 8 * x) * 2);
+    } else {
+      const int piece = lane % 16;
+      const uint8_t *at = vb + (32 * b + 16 * half + 8 * x + piece / 4) * L::kVStride +
+                          (32 * i + 16 * ((lane >> 4) & 1) + 4 * (piece % 4)) * 2;
+      const uint2 v0 = lds_read_transposed(at), v1 = lds_read_transposed(at + 4 * L::kVStride);
+      return make_uint4(v0.x, v0.y, v1.x, v1.y);
+    }
+  };
+  // STEPS operands, each used for every block of rows, with `work` (step, block) behind each matrix
+  // instruction; the reads run on into the operands of the next chain.  The walls hold the order:
+  // left alone the compiler reads all operands at once, for which there are no registers, or gathers
+  // the vector work behind the products.
+  uint4 ring[AHEAD + 1];
+  static_assert(STEPS % (AHEAD + 1) == 0, "a chain leaves the ring where the next one starts");
+  auto prime = [&](auto operand) {
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) ring[n] = operand(n);
+  };
+  auto chain = [&](auto operand, auto next_operand, auto product, auto work) {
+    sched_wall();
+    auto step = [&](auto at) {
+      constexpr int n = decltype(at)::value;
+      ring[(n + AHEAD) % (AHEAD + 1)] = n + AHEAD < STEPS ? operand(n + AHEAD) : next_operand(n + AHEAD - STEPS);
+      auto block = [&](auto bx) {
+        product(n, decltype(bx)::value, __builtin_bit_cast(bf16x8, ring[n % (AHEAD + 1)]));
+        work(std::integral_constant<int, n * RT + decltype(bx)::value>{});
+        sched_wall();
       };
-#pragma unroll
-      for (int i = 0; i < KU; ++i) {
-        const int u = tid + i * kThreads, token = u / (DP / 16), piece = u % (DP / 16);
-        const int64_t pg = group_page(__builtin_amdgcn_readfirstlane(token / 16));
-        kr[i] = make_uint4(0, 0, 0, 0);
-        if (pg >= 0 && 16 * piece < D)
-          kr[i] = *reinterpret_cast<const uint4 *>(a.c.kc + (pg * a.c.P + (int)((j0 + token) & (a.c.P - 1))) * D + 16 * piece);
-      }
-#pragma unroll
-      for (int i = 0; i < VU; ++i) {
-        const int u = tid + i * kThreads, d = u % DP;
-        const int g = __builtin_amdgcn_readfirstlane(u / DP);
-        const int64_t pg = group_page(g);
-        vr[i] = make_uint4(0, 0, 0, 0);
-        if (pg >= 0 && d < D)
-          vr[i] = *reinterpret_cast<const uint4 *>(a.c.vc + pg * a.c.P * D + ((int64_t)((j0 + 16 * g) & (a.c.P - 1)) * D + d * 16));
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int64_t pg = group_page(2 * i + half);
-        ks[i] = pg >= 0 ? a.c.ks[pg] : 0.0f;
-        vs[i] = pg >= 0 ? a.c.vs[pg] : 0.0f;
-      }
-    } else {
-      const int64_t j = j0 + lane;
-      bool on = j < rows.keys;
-      if (on && a.mask) on = a.mask[s * a.mask_stride + j] != 0;
-      seen_bits = __ballot(on);
-#pragma unroll
-      for (int i = 0; i < 2 * KU; ++i) {
-        const int u = tid + i * kThreads, token = u / (DP / 8), piece = u % (DP / 8);
-        kr[i] = make_uint4(0, 0, 0, 0);
-        if ((seen_bits >> token & 1) && 8 * piece < D)
-          kr[i] = *reinterpret_cast<const uint4 *>(a.k.p + s * a.k.bs + (j0 + token) * a.k.ts + h * a.k.hs + 8 * piece);
-        vr[i] = make_uint4(0, 0, 0, 0);
-        if ((seen_bits >> token & 1) && 8 * piece < D)
-          vr[i] = *reinterpret_cast<const uint4 *>(a.v.p + s * a.v.bs + (j0 + token) * a.v.ts + h * a.v.hs + 8 * piece);
-      }
-    }
+      static_for<RT>(block);
+    };
+    static_for<STEPS>(step);
   };
-  auto stage = [&](uint8_t *buf) {
-    uint8_t *kb = buf, *vb = buf + L::kKeys;
-    if constexpr (CACHED) {
+  // f(i) for the part of `count` pieces, spread over instructions [from, until) of a chain, that
+  // belongs to instruction `at`
+  auto share = [](auto at, int from, int until, int count, auto f) {
+    const int n = decltype(at)::value, N = until - from;
+    if (n < from || n >= until) return;
 #pragma unroll
-      for (int i = 0; i < KU; ++i) {
-        const int u = tid + i * kThreads, token = u / (DP / 16), piece = 2 * (u % (DP / 16)), sw = swizzle(token);
-        *reinterpret_cast<uint4 *>(kb + token * DP * 2 + ((piece ^ sw) * 16)) = codes8_to_bf16(kr[i].x, kr[i].y);
-        *reinterpret_cast<uint4 *>(kb + token * DP * 2 + (((piece + 1) ^ sw) * 16)) = codes8_to_bf16(kr[i].z, kr[i].w);
-      }
-#pragma unroll
-      for (int i = 0; i < VU; ++i) {
-        const int u = tid + i * kThreads, d = u % DP, g = u / DP;
-        uint4 *to = reinterpret_cast<uint4 *>(vb + d * L::kVStride + g * 32);
-        to[0] = codes8_to_bf16(vr[i].x, vr[i].y);
-        to[1] = codes8_to_bf16(vr[i].z, vr[i].w);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 2 * KU; ++i) {
-        const int u = tid + i * kThreads, token = u / (DP / 8), piece = u % (DP / 8);
-        *reinterpret_cast<uint4 *>(kb + token * DP * 2 + ((piece ^ swizzle(token)) * 16)) = kr[i];
-        *reinterpret_cast<uint4 *>(vb + token * L::kVStride + piece * 16) = vr[i];
-      }
-    }
+    for (int i = (n - from) * count / N; i < (n - from + 1) * count / N; ++i) f(i);
   };
 
-  float ks_now[2], vs_now[2];
-  uint64_t bits = ~0ull;
-  if (tiles > 0) {
-    fetch(0);
-    stage(lds);
-    bits = seen_bits;
+  // Scores of a half tile: a lane has 16 tokens of one 16-token group, with one scale c.  States'
+  // scores start from their bias.  Where a cache's tokens lie beyond the row's end they become
+  // -infinity, with the scale applied here, so that a scale that is 0 or NaN reaches only what is
+  // seen; a NaN scale of the values goes by the scores.
+  struct Scores {
+    f32x16 st[RT];
+    float c[RT], v[RT], top[RT];
+  };
+  auto begin = [&](Scores &z, int t, int b, float ks, float vs) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) ks_now[i] = ks[i], vs_now[i] = vs[i];
-  }
-  for (int t = 0; t < tiles; ++t) {
-    const uint8_t *kb = lds + (t & 1) * L::kBuffer, *vb = kb + L::kKeys;
-    __syncthreads();
-    if (t + 1 < tiles) fetch(t + 1);
-    const int64_t j0 = c0 + (int64_t)t * kTile;
-    if (j0 < end_max) {
-      // S^T: row i = 8 x + 4 y + z of a 32-token block is token 16 y + 4 x + z
-      const int token = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
-      f32x16 st[2];
+    for (int x = 0; x < RT; ++x) {
+      if constexpr (CACHED) {
+        z.st[x] = f32x16{};
+      } else {
+        const float4 *p = reinterpret_cast<const float4 *>(bias + (t & 3) * kTile + 32 * b + 16 * half);
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        st[b] = f32x16{};
-        const uint8_t *row = kb + (32 * b + token) * DP * 2;
-        const int sw = swizzle(token);
-#pragma unroll
-        for (int i = 0; i < DP / 16; ++i)
-          if (16 * i < D) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(row + (((2 * i + half) ^ sw) * 16));
-            st[b] = mfma32(__builtin_bit_cast(bf16x8, u), q[i], st[b]);
-          }
-      }
-      float c[2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) c[b] = CACHED ? c_all * ks_now[b] : c_all;
-      // unseen places: beyond a row's end, or masked
-      const bool masked = j0 + kTile > end_min || (!CACHED && bits != ~0ull);
-      uint32_t on[2] = {0xFFFFu, 0xFFFFu};
-      if (masked) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const int64_t left = end - (j0 + 32 * b + 16 * half);
-          on[b] = left >= 16 ? 0xFFFFu : left <= 0 ? 0u : (1u << left) - 1;
-          if (!CACHED) on[b] &= (uint32_t)(bits >> (32 * b + 16 * half));
+        for (int e = 0; e < 4; ++e) {
+          const float4 f = p[e];
+          z.st[x][4 * e] = f.x, z.st[x][4 * e + 1] = f.y, z.st[x][4 * e + 2] = f.z, z.st[x][4 * e + 3] = f.w;
         }
       }
-      float top = -FLT_MAX;
+      z.c[x] = CACHED ? c_all * ks : c_all;
+      z.v[x] = CACHED ? vs : 1.0f;
+    }
+  };
+  int least = end_min[0];  // that any row of the wave sees
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        float x = -FLT_MAX;
-        if (masked) {
+  for (int x = 1; x < RT; ++x) least = end_min[x] < least ? end_min[x] : least;
+  auto hide_unseen = [&](Scores &z, int t, int b) {
+    const int j0 = c0 + t * kTile + 32 * b;
+    if (CACHED && j0 + 32 > least)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x = maxf(x, (on[b] >> e & 1) ? st[b][e] : -FLT_MAX);
-          if (on[b]) top = maxf(top, x * c[b]);
-        } else {
+      for (int x = 0; x < RT; ++x) {
+        const int left = end[x] - (j0 + 16 * half);
+        const uint32_t on = left >= 16 ? 0xFFFFu : left <= 0 ? 0u : (1u << left) - 1;
+        const float bad = z.v[x] - z.v[x];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x = maxf(x, st[b][e]);
-          top = maxf(top, x * c[b]);
-        }
+        for (int e = 0; e < 16; ++e) z.st[x][e] = (on >> e & 1) ? __builtin_fmaf(z.st[x][e], z.c[x], bad) : -INFINITY;
+        z.c[x] = 1.0f;
+        z.v[x] = bad == 0.0f ? z.v[x] : 1.0f;
       }
-      top = across32(top, maxf);
-      // the running maximum moves only where it has to: up to 2^8 above it a weight is as exact
-      if (__any(top > m + 8.0f)) {
-        const float to = maxf(m, top), shrink = exp2_fast(m - to);
-        m = to;
-        l *= shrink;
+  };
+  // maximum of a lane's scores, two at a time: piece n of 8 RT
+  auto two_maxima = [&](Scores &z, int n) {
+    const int x = n % RT, y = n / RT;
+    const float t0 = maxf(z.st[x][2 * y], z.st[x][2 * y + 1]);
+    z.top[x] = y == 0 ? t0 : maxf(z.top[x], t0);
+    asm volatile("" : "+v"(z.top[x]));
+  };
+  // The running maximum moves only where it has to: a weight up to 2^8 is as exact as one up to 1.
+  auto follow_maximum = [&](const Scores &z) {
+    bool above = false;
+    float top[RT];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+      top[x] = z.top[x] * z.c[x];
+      above = above || top[x] > m[x] + 8.0f;
+    }
+    if (__any(above))
+#pragma unroll
+      for (int x = 0; x < RT; ++x) {
+        const float to = maxf(m[x], across32(maxf(top[x], -FLT_MAX), maxf)), shrink = exp2_fast(m[x] - to);
+        m[x] = to;
+        l[x][0] *= shrink;
+        l[x][1] *= shrink;
 #pragma unroll
         for (int i = 0; i < DP / 32; ++i)
-          if (32 * i < D) o[i] *= shrink;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[x][i][e] *= shrink;
       }
-      bf16x8 p[2][2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        float w[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float x = exp2_fast(__builtin_fmaf(st[b][e], c[b], -m));
-          if (masked) x = (on[b] >> e & 1) ? x : 0.0f;
-          l += x;
-          w[e] = CACHED ? x * vs_now[b] : x;
-          if (CACHED && masked) w[e] = (on[b] >> e & 1) ? w[e] : 0.0f;
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          p[b][e] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(w[8 * e], w[8 * e + 1]), pack_bf16(w[8 * e + 2], w[8 * e + 3]),
-                                                         pack_bf16(w[8 * e + 4], w[8 * e + 5]), pack_bf16(w[8 * e + 6], w[8 * e + 7])));
+  };
+  uint4 w[RT][2];  // weights in the operand order of the second product
+  // Two scores to weights: piece n of 8 RT + 1, all blocks' first 8 tokens before their last 8.  The
+  // exponentials of a piece come with the sums and conversions of the one before, whose results
+  // they would otherwise wait for.
+  float e0 = 0.0f, e1 = 0.0f;
+  auto two_weights = [&](const Scores &z, int n) {
+    const float p0 = e0, p1 = e1;
+    if (n < 8 * RT) {
+      const int x = n / 4 % RT, y = n / (4 * RT) * 4 + n % 4;
+      e0 = exp2_fast(__builtin_fmaf(z.st[x][2 * y], z.c[x], -m[x]));
+      e1 = exp2_fast(__builtin_fmaf(z.st[x][2 * y + 1], z.c[x], -m[x]));
+    }
+    if (n > 0) {
+      const int k = n - 1, x = k / 4 % RT, y = k / (4 * RT) * 4 + k % 4;
+      uint32_t u;
+      if constexpr (CACHED) {
+        l[x][0] += p0;
+        l[x][1] += p1;
+        u = pack_bf16(p0 * z.v[x], p1 * z.v[x]);
+      } else {  // the sum of the weights as they are used
+        u = pack_bf16(p0, p1);
+        l[x][n % 2] = add_pair(u, l[x][n % 2]);
       }
-      // O^T: a lane's weights 8 e .. 8 e + 7 are tokens 32 b + 16 half + 8 e ..
+      asm volatile("" : "+v"(u), "+v"(l[x][0]), "+v"(l[x][1]));  // here, not where the weights are used
+      uint4 &to = w[x][y / 4];
+      (y % 4 == 0 ? to.x : y % 4 == 1 ? to.y : y % 4 == 2 ? to.z : to.w) = u;
+    }
+    asm volatile("" : "+v"(e0), "+v"(e1));
+  };
+  auto output_product = [&](int n, int x, bf16x8 u) {
+    const int i = n % (DP / 32);
+    o[x][i] = mfma32(u, __builtin_bit_cast(bf16x8, w[x][n / (DP / 32)]), o[x][i]);
+  };
+  constexpr int kWeights = 8 * RT + 1, kMaxima = 8 * RT, kLength = STEPS * RT;
+  // weights left for the first half of the second chain, whose products need only the first half
+  constexpr int kLate = kWeights * 5 / 16;
+
+  // Weights and outputs of a half tile (b of values vb), scores of the next (b_next of tile t_next:
+  // keys kb; after it, operands from `following`), with `pieces` of staging in the second chain.
+  auto half_tile = [&](Scores &now, Scores &next, const uint8_t *vb, int b, const uint8_t *kb, int t_next, int b_next,
+                       auto following, auto pieces, auto stage) {
+    auto values = [&](int n) { return value_operand(vb, b, n); };
+    chain([&](int n) { return key_operand(kb, b_next, n); }, values,
+          [&](int n, int x, bf16x8 k) { next.st[x] = mfma32(k, q[x][n], next.st[x]); },
+          [&](auto at) { share(at, 0, kLength, kWeights - kLate, [&](int n) { two_weights(now, n); }); });
+    hide_unseen(next, t_next, b_next);
+    chain(values, following, output_product, [&](auto at) {
+      share(at, 0, kLength / 2, kLate, [&](int n) { two_weights(now, kWeights - kLate + n); });
+      share(at, kLength / 8, kLength, kMaxima, [&](int n) { two_maxima(next, n); });
+      share(at, kLength / 2, kLength, decltype(pieces)::value, stage);
+    });
+    follow_maximum(next);
+  };
+
+  // scale of a lane's half of the tokens of half tile b, from the lanes that hold the groups' scales
+  auto scale_of = [&](float v, int b) {
+    const float x0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 2 * b));
+    const float x1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 2 * b + 1));
+    return half ? x1 : x0;
+  };
+  Scores sa, sb;
+  float ks0 = 0.0f, ks1 = 0.0f, vs0 = 0.0f, vs1 = 0.0f;  // scales of this tile's groups and the next's
+  auto bits_of = [&](uint32_t mask) { return CACHED ? ~0ull : __ballot(mask != 0); };
+  uint64_t bits = ~0ull;  // seen places of the tile after this one
+  if (tiles > 0) {
+    // keys 0 and 1 and values 0 into LDS, values 1 and keys 2 under way
+    if constexpr (CACHED) look_up(0);
+    load_keys(0);
+    load_mask(0);
+    at_v = at_k;
+    scale_v = scale_k;
+    if constexpr (CACHED) look_up(1);
+#pragma unroll
+    for (int i = 0; i < (CACHED ? KU : VU); ++i) hold.k[i] = in.k[i];
+    hold.mask = in.mask;
+    ks0 = in.ks;
+    load(0);
+    const uint64_t bits0 = bits_of(hold.mask);
+    write_bias(0);
+    if constexpr (!CACHED) clear_rows(hold.k, bits0);
+#pragma unroll
+    for (int n = 0; n < kKeyPieces; ++n) stage_key(keys_at, n);
+    hold = in;
+    bits = bits_of(hold.mask);
+    ks1 = in.ks;
+    vs0 = in.vs;
+    load(1);
+    write_bias(1);
+    if constexpr (!CACHED) {
+      clear_rows(hold.k, bits);
+      clear_rows(hold.v, bits0);
+    }
+#pragma unroll
+    for (int n = 0; n < kKeyPieces; ++n) stage_key(keys_at + L::kKeys, n);
+#pragma unroll
+    for (int n = 0; n < kValuePieces; ++n) stage_value(values_at, n);
+    __syncthreads();
+    begin(sa, 0, 0, scale_of(ks0, 0), scale_of(vs0, 0));
+    auto first = [&](int n) { return key_operand(keys_at, 0, n); };
+    prime(first);
+    chain(first, [&](int n) { return key_operand(keys_at, 1, n); },
+          [&](int n, int x, bf16x8 k) { sa.st[x] = mfma32(k, q[x][n], sa.st[x]); }, [](auto) {});
+    hide_unseen(sa, 0, 0);
+#pragma unroll
+    for (int n = 0; n < kMaxima; ++n) two_maxima(sa, n);
+    follow_maximum(sa);
+  }
+  // Tile t, with its buffers known to the compiler.
+  auto tile = [&](int t, auto parity) {
+    constexpr int even = decltype(parity)::value;
+    // values t and keys t + 1 are in LDS (behind the barrier), values t + 1 and keys t + 2 under way
+    const uint8_t *vb = values_at + even * L::kValues;
+    uint8_t *k0 = keys_at + even * L::kKeys, *k1 = keys_at + (1 - even) * L::kKeys;
+    __syncthreads();
+    begin(sb, t, 1, scale_of(ks0, 1), scale_of(vs0, 1));
+    hold = in;
+    load(t + 2);
+    write_bias(t + 2);
+    if constexpr (!CACHED) {
+      clear_rows(hold.v, bits);
+      bits = bits_of(hold.mask);
+      clear_rows(hold.k, bits);
+    }
+    half_tile(sa, sb, vb, 0, k0, t, 1, [&](int n) { return key_operand(k1, 0, n); }, ValuePieces{},
+              [&](int n) { stage_value(values_at + (1 - even) * L::kValues, n); });
+    vs1 = hold.vs;
+    __syncthreads();
+    begin(sa, t + 1, 0, scale_of(ks1, 0), scale_of(vs1, 0));
+    half_tile(sb, sa, vb, 1, k1, t + 1, 0, [&](int n) { return key_operand(k1, 1, n); }, KeyPieces{},
+              [&](int n) { stage_key(k0, n); });
+    ks0 = ks1, vs0 = vs1, ks1 = hold.ks;
+  };
+  for (int t = 0; t < tiles; t += 2) {
+    tile(t, std::integral_constant<int, 0>{});
+    if (t + 1 == tiles) break;
+    tile(t + 1, std::integral_constant<int, 1>{});
+  }
+#pragma unroll
+  for (int x = 0; x < RT; ++x) {
+    const float sum = across32(l[x][0] + l[x][1], [](float y, float z) { return y + z; });
+    if (!live[x]) continue;
+    // a lane holds channels 32 i + 8 y + 4 half + z of its row
+    if (sp.splits > 1) {
+      const int64_t at = (((int64_t)part * a.seqs + s) * a.Hk + h) * (a.max_new * G) + r0 + (wave * RT + x) * 32 + col;
+      if (half == 0) sp.ml[at] = make_float2(m[x], sum);
 #pragma unroll
       for (int i = 0; i < DP / 32; ++i)
-        if (32 * i < D) {
 #pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              uint4 u;
-              if constexpr (CACHED) {
-                u = *reinterpret_cast<const uint4 *>(vb + (32 * i + col) * L::kVStride + (32 * b + 16 * half + 8 * e) * 2);
-              } else {
-                const int piece = lane % 16;
-                const uint8_t *at = vb + (32 * b + 16 * half + 8 * e + piece / 4) * L::kVStride +
-                                    (32 * i + 16 * ((lane >> 4) & 1) + 4 * (piece % 4)) * 2;
-                const uint2 x = lds_read_transposed(at), y = lds_read_transposed(at + 4 * L::kVStride);
-                u = make_uint4(x.x, x.y, y.x, y.y);
-              }
-              o[i] = mfma32(__builtin_bit_cast(bf16x8, u), p[b][e], o[i]);
-            }
+        for (int y = 0; y < 4; ++y) {
+          const int d = 32 * i + 8 * y + 4 * half;
+          if (d < D)
+            *reinterpret_cast<float4 *>(sp.o + at * D + d) =
+                make_float4(o[x][i][4 * y], o[x][i][4 * y + 1], o[x][i][4 * y + 2], o[x][i][4 * y + 3]);
         }
+      continue;
     }
-    if (t + 1 < tiles) {
-      stage(lds + ((t + 1) & 1) * L::kBuffer);
-      bits = seen_bits;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) ks_now[i] = ks[i], vs_now[i] = vs[i];
-    }
-  }
-  l = across32(l, [](float x, float y) { return x + y; });
-  if (!live) return;
-  // a lane holds channels 32 i + 8 x + 4 half + z of its row
-  if (sp.splits > 1) {
-    const int64_t at = ((part * a.seqs + s) * a.Hk + h) * (a.max_new * G) + r;
-    if (half == 0) sp.ml[at] = make_float2(m, l);
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+    uint16_t *out = a.out + ((rows.q0 + qi[x]) * a.Hq + hq[x]) * D;
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int d = 32 * i + 8 * x + 4 * half;
+      for (int y = 0; y < 4; ++y) {
+        const int d = 32 * i + 8 * y + 4 * half;
         if (d < D)
-          *reinterpret_cast<float4 *>(sp.o + at * D + d) = make_float4(o[i][4 * x], o[i][4 * x + 1], o[i][4 * x + 2], o[i][4 * x + 3]);
+          *reinterpret_cast<uint2 *>(out + d) = make_uint2(pack_bf16(o[x][i][4 * y] * inv, o[x][i][4 * y + 1] * inv),
+                                                          pack_bf16(o[x][i][4 * y + 2] * inv, o[x][i][4 * y + 3] * inv));
       }
-    return;
   }
-  const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-  uint16_t *out = a.out + ((rows.q0 + qi) * a.Hq + hq) * D;
-#pragma unroll
-  for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int d = 32 * i + 8 * x + 4 * half;
-      if (d < D)
-        *reinterpret_cast<uint2 *>(out + d) = make_uint2(pack_bf16(o[i][4 * x] * inv, o[i][4 * x + 1] * inv),
-                                                        pack_bf16(o[i][4 * x + 2] * inv, o[i][4 * x + 3] * inv));
-    }
 }
 
-template <bool CACHED, int DP>
+template <bool CACHED, int DP, int RT, int WAVES>
 hipError_t launch(const AttnArgs &a, const Split &sp, hipStream_t s) {
   static std::atomic<uint64_t> raised{0};
-  const size_t lds = 2 * (size_t)Lds<CACHED, DP>::kBuffer;
-  hipError_t e = allow_dynamic_lds(attention_tile_kernel<CACHED, DP>, lds, raised);
+  const size_t lds = Lds<CACHED, DP>::kBytes;
+  hipError_t e = allow_dynamic_lds(attention_tile_kernel<CACHED, DP, RT, WAVES>, lds, raised);
   if (e != hipSuccess) return e;
-  const int64_t row_tiles = (a.max_new * (a.Hq / a.Hk) + kRows - 1) / kRows;
-  attention_tile_kernel<CACHED, DP><<<dim3((unsigned)(a.Hk * row_tiles * sp.splits), (unsigned)a.seqs), kThreads, lds, s>>>(
-      a, sp, (int)row_tiles);
+  const int rows = 32 * RT * WAVES;
+  const int64_t row_tiles = (a.max_new * (a.Hq / a.Hk) + rows - 1) / rows;
+  attention_tile_kernel<CACHED, DP, RT, WAVES>
+      <<<dim3((unsigned)(a.Hk * row_tiles * sp.splits), (unsigned)a.seqs), 64 * WAVES, lds, s>>>(a, sp, (int)row_tiles);
   return hipGetLastError();
 }
 
 template <bool CACHED>
-hipError_t launch_size(const AttnArgs &a, const Split &sp, hipStream_t s) {
-  if (a.D <= 64) return launch<CACHED, 64>(a, sp, s);
-  if (a.D <= 128) return launch<CACHED, 128>(a, sp, s);
-  return launch<CACHED, 256>(a, sp, s);
+hipError_t launch_size(const AttnArgs &a, const Split &sp, int rows, hipStream_t s) {
+  if (a.D <= 64) return launch<CACHED, 64, 1, 4>(a, sp, s);
+  if (a.D <= 128) return rows > 128 ? launch<CACHED, 128, 1, 8>(a, sp, s) : launch<CACHED, 128, 1, 4>(a, sp, s);
+  return launch<CACHED, 256, 1, 4>(a, sp, s);
 }
 
 }  // namespace
 
-int attention_tile_rows() { return kRows; }
-
-hipError_t launch_attention_tile(bool cached, const AttnArgs &a, const Split &sp, hipStream_t s) {
-  return cached ? launch_size<true>(a, sp, s) : launch_size<false>(a, sp, s);
+hipError_t launch_attention_tile(bool cached, const AttnArgs &a, const Split &sp, int rows, hipStream_t s) {
+  return cached ? launch_size<true>(a, sp, rows, s) : launch_size<false>(a, sp, rows, s);
 }
 
 }  // namespace fq
