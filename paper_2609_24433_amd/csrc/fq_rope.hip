@@ -44,14 +44,20 @@ __device__ __forceinline__ uint4 pack8(const float *v) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-__device__ __forceinline__ void load_head(const uint16_t *x, const Place &p, float (&v)[16]) {
-  uint4 u0 = make_uint4(0, 0, 0, 0), u1 = u0;
-  if (p.in) {
-    u0 = *reinterpret_cast<const uint4 *>(x + p.a);
-    u1 = *reinterpret_cast<const uint4 *>(x + p.b);
+struct Raw {
+  uint4 a, b;
+};
+__device__ __forceinline__ Raw load_raw(const uint16_t *x, const Place &p, bool on) {
+  Raw r{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+  if (on && p.in) {
+    r.a = *reinterpret_cast<const uint4 *>(x + p.a);
+    r.b = *reinterpret_cast<const uint4 *>(x + p.b);
   }
-  unpack8(u0, v);
-  unpack8(u1, v + 8);
+  return r;
+}
+__device__ __forceinline__ void unpack(const Raw &r, float (&v)[16]) {
+  unpack8(r.a, v);
+  unpack8(r.b, v + 8);
 }
 
 __device__ __forceinline__ void load_weight(const float *w, const Place &p, float (&g)[16]) {
@@ -129,7 +135,7 @@ __device__ __forceinline__ void rope_heads(const uint16_t *x, int64_t hs, uint16
   load_weight(w, p, g);
   for (int h = slice; h < H; h += S) {
     float v[16];
-    load_head(x + h * hs, p, v);
+    unpack(load_raw(x + h * hs, p, true), v);
     norm_rotate<L>(v, w != nullptr, g, cs, p, r.interleaved, r.eps, D);
     store_head(y + (int64_t)h * D, p, v);
   }
@@ -214,15 +220,17 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t *lds) {
   return v;
 }
 
-// Workgroups [0, kv_items): one page of one sequence and head, keys or values; all of the page's
-// new tokens are read twice (the second time from a cache) for the scale and then the codes.
-// The others: the query heads of the new tokens.
-template <int L>
+// Workgroups [0, kv_items): one page of one sequence and head, keys or values.  The page's new tokens
+// are read once, NP a lane group, and stay in registers as they came: their largest value gives the
+// scale, then they become codes.  The others: the query heads of the new tokens.
+template <int L, int NP>
 __global__ __launch_bounds__(kThreads) void cache_append_kernel(Cache c, Batch b, Heads k, Heads v, Heads q, int Hq,
                                                                 int Sq, int64_t kv_items, int pages_per_seq,
                                                                 int64_t q_blocks, Rope r, int64_t T,
                                                                 uint16_t *__restrict__ q_out) {
-  extern __shared__ __align__(16) uint8_t tile[];  // values: the page's new codes, [P/16][D][16]
+  // values: the page's new codes [P/16][D][16], 16 bytes more every 16 channels (a token's channels
+  // are written 16 apart by the lanes: the gap moves them to banks of their own)
+  extern __shared__ __align__(16) uint8_t tile[];
   __shared__ uint32_t red[kThreads / 64];
   constexpr int NG = kThreads / L;
   const int D = c.D, P = c.P, m = threadIdx.x % L, grp = threadIdx.x / L;
@@ -248,37 +256,43 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(Cache c, Batch b
   const int64_t pw = first / P + item / c.H % pages_per_seq, lo = pw * P;
   const int64_t s0 = lo > first ? lo : first, s1 = lo + P < sp.end ? lo + P : sp.end;
   if (sp.n <= 0 || s1 <= s0) return;
-  const int held = (int)(first > lo ? first - lo : 0);
+  const int held = (int)(first > lo ? first - lo : 0), from = (int)(s0 - lo), to = (int)(s1 - lo);
   const int64_t page = page_of(b, c.pages, s, pw) * c.H + h;
   const Place pl = keys ? p : place_of(m, D, 0, 0);
+  float *scale_at = (keys ? c.ks : c.vs) + page;
+  const float old = held ? *scale_at : 0.0f;
+  const int64_t t0 = sp.row + (s0 - sp.begin);  // token of slot s0
+  const Heads &in = keys ? k : v;
+  Raw raw[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int o = grp + i * NG;
+    raw[i] = load_raw(in.p + (t0 + o) * in.ts + h * in.hs, pl, from + o < to);
+  }
   float g[16];
   load_weight(keys ? r.kw : nullptr, pl, g);
-
-  auto token = [&](int64_t slot, float(&x)[16]) {
-    const int64_t t = sp.row + (slot - sp.begin);
-    if (keys) {
+  auto value = [&](int i, float(&x)[16]) {
+    unpack(raw[i], x);
+    const int o = grp + i * NG;
+    if (keys && from + o < to) {
       float2 cs[8];
-      load_angles(r, pl, m, r.positions ? r.positions[t] : slot, cs);
-      load_head(k.p + t * k.ts + h * k.hs, pl, x);
+      load_angles(r, pl, m, r.positions ? r.positions[t0 + o] : s0 + o, cs);
       norm_rotate<L>(x, r.kw != nullptr, g, cs, pl, r.interleaved, r.eps, D);
-    } else {
-      load_head(v.p + t * v.ts + h * v.hs, pl, x);
     }
   };
 
   uint32_t top = 0;
-  for (int64_t slot = s0 + grp; slot < s1; slot += NG) {
-    float x[16];
-    token(slot, x);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const uint32_t a = abs_bits(x[i]);
+  for (int i = 0; i < NP; ++i) {
+    float x[16];
+    value(i, x);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const uint32_t a = abs_bits(x[e]);
       top = a > top ? a : top;
     }
   }
-  top = block_max(top, red);
-  float *scale_at = (keys ? c.ks : c.vs) + page;
-  const float old = held ? *scale_at : 0.0f;
+  top = block_max(top, red);  // every thread has read the old scale
   float scale = __uint_as_float(top) / 127.0f;
   bool bad = top >= 0x7F800000u;
   if (held) {
@@ -289,7 +303,6 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(Cache c, Batch b
   const bool grew = held && !bad && scale != old;
   const float inv = scale > 0.0f && !bad ? 1.0f / scale : 0.0f;
   const float ratio = scale > 0.0f ? old / scale : 0.0f;
-  __syncthreads();  // every thread has read the old scale
   if (threadIdx.x == 0) *scale_at = bad ? __uint_as_float(0x7FC00000u) : scale;
 
   if (keys) {
@@ -300,52 +313,55 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(Cache c, Batch b
         const uint4 o = *w;
         *w = make_uint4(rescale4(o.x, ratio), rescale4(o.y, ratio), rescale4(o.z, ratio), rescale4(o.w, ratio));
       }
-    for (int64_t slot = s0 + grp; slot < s1; slot += NG) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int o = from + grp + i * NG;
+      if (o >= to) continue;
       float x[16];
-      token(slot, x);
+      value(i, x);
+      if (!pl.in) continue;  // (after the norm's exchange)
       uint32_t w[4] = {0, 0, 0, 0};
       if (!bad)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) w[i / 4] |= ((uint32_t)code_of(x[i], inv) & 0xFFu) << (8 * (i % 4));
-      int8_t *row = base + (slot - lo) * D;
-      if (pl.in) {
-        *reinterpret_cast<uint2 *>(row + pl.a) = make_uint2(w[0], w[1]);
-        *reinterpret_cast<uint2 *>(row + pl.b) = make_uint2(w[2], w[3]);
-      }
+        for (int e = 0; e < 16; ++e) w[e / 4] |= ((uint32_t)code_of(x[e], inv) & 0xFFu) << (8 * (e % 4));
+      int8_t *row = base + o * D;
+      *reinterpret_cast<uint2 *>(row + pl.a) = make_uint2(w[0], w[1]);
+      *reinterpret_cast<uint2 *>(row + pl.b) = make_uint2(w[2], w[3]);
     }
     return;
   }
-  for (int64_t slot = s0 + grp; slot < s1; slot += NG) {
-    float x[16];
-    token(slot, x);
-    const int o = (int)(slot - lo);
-    uint8_t *to = tile + (o / 16) * D * 16 + o % 16;
-    if (pl.in)
+  const int group_bytes = 17 * D;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) to[(16 * m + i) * 16] = bad ? 0 : (uint8_t)code_of(x[i], inv);
+  for (int i = 0; i < NP; ++i) {
+    const int o = from + grp + i * NG;
+    if (o >= to || !pl.in) continue;
+    float x[16];
+    value(i, x);
+    uint8_t *at = tile + (o / 16) * group_bytes + m * 272 + o % 16;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) at[16 * e] = bad ? 0 : (uint8_t)code_of(x[e], inv);
   }
   __syncthreads();
   // 16 tokens of one channel an item: earlier codes, then the new ones, then zeros
-  const int from = (int)(s0 - lo), to = (int)(s1 - lo);
   const int g0 = grew ? 0 : from / 16, g1 = (to + 15) / 16;
   uint4 *base = reinterpret_cast<uint4 *>(c.vc + page * P * D);
   for (int i = g0 * D + threadIdx.x; i < g1 * D; i += kThreads) {
-    const int t0 = i / D * 16;
+    const int group = i / D, d = i - group * D, t = group * 16;
     uint32_t w[4] = {0, 0, 0, 0};
-    if (t0 < held) {
+    if (t < held) {
       const uint4 o = base[i];
       w[0] = o.x, w[1] = o.y, w[2] = o.z, w[3] = o.w;
       if (grew)
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = rescale4(w[j], ratio);
     }
-    const uint4 n = reinterpret_cast<const uint4 *>(tile)[i];
+    const uint4 n = *reinterpret_cast<const uint4 *>(tile + group * group_bytes + d * 16 + d / 16 * 16);
     const uint32_t nw[4] = {n.x, n.y, n.z, n.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int o = t0 + 4 * j + e;
+        const int o = t + 4 * j + e;
         const uint32_t mask = 0xFFu << (8 * e);
         if (o >= from) w[j] = (w[j] & ~mask) | (o < to ? nw[j] & mask : 0u);
       }
@@ -353,55 +369,105 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(Cache c, Batch b
   }
 }
 
-// One 16-token group of one head: codes times scales, the rows of [first, last), zeros beyond.
+// 64 tokens of one head: codes times scales, the rows of [first, last), zeros beyond.  All of a
+// thread's loads (NJ pieces of 8 channels, NJ / 2 of 16 tokens) are in flight together: the kernel
+// waits three times on memory, for the bounds, the pages and the codes, whatever it moves.
+constexpr int kReadTokens = 64;
+template <int NJ>
 __global__ __launch_bounds__(kThreads) void cache_read_kernel(Cache c, const int32_t *__restrict__ pt, int64_t width,
                                                               const int32_t *__restrict__ first,
-                                                              const int32_t *__restrict__ last, int groups,
+                                                              const int32_t *__restrict__ last, int windows,
                                                               int64_t max_tokens, uint16_t *__restrict__ k_out,
                                                               uint16_t *__restrict__ v_out) {
-  __shared__ __align__(16) int8_t vt[256 * 16];
-  const int D = c.D, P = c.P;
+  // values [4][D][16], 16 bytes more every 8 channels: lanes that read a token's channels, 8 apart,
+  // meet banks of their own
+  __shared__ __align__(16) uint8_t vt[kReadTokens / 16 * 18 * 32 * NJ];
+  __shared__ float vscale[kReadTokens / 16];
+  constexpr int NV = NJ > 1 ? NJ / 2 : 1;
+  const int D = c.D, lp = 31 - __builtin_clz(c.P), in_page = c.P - 1;
+  const uint32_t per = D / 8, by_per = ((1u << 20) + per - 1) / per, by_d = ((1u << 20) + D - 1) / D;  // x / per = x by_per >> 20
   const int h = blockIdx.x % c.H;
-  const int64_t s = blockIdx.x / c.H / groups;
+  const int64_t s = blockIdx.x / c.H / windows;
   const int64_t f = first[s] < 0 ? 0 : first[s], e = last[s];
-  const int64_t t0 = (f / 16 + blockIdx.x / c.H % groups) * 16;  // first token of the cache's group
-  const int64_t w = t0 / P;
-  const bool there = w < width && t0 < e;
-  int64_t page = there ? pt[s * width + w] : 0;
-  page = (page < 0 ? 0 : page >= c.pages ? c.pages - 1 : page) * c.H + h;
-  const int o = (int)(t0 % P);
-  const float ks = there ? c.ks[page] : 0.0f, vs = there ? c.vs[page] : 0.0f;
-  if (there && v_out)
-    for (int i = threadIdx.x; i < D; i += kThreads)
-      reinterpret_cast<uint4 *>(vt)[i] = reinterpret_cast<const uint4 *>(c.vc + page * P * D + (int64_t)(o / 16) * D * 16)[i];
+  const int64_t t0 = f / 16 * 16 + (int64_t)(blockIdx.x / c.H % windows) * kReadTokens;
+  // Page (times heads) of a token, or of the last one where it is beyond: loads need no branch.
+  const int64_t there = (e < width << lp ? e : width << lp) - 1;
+  if (there < 0) {
+    // nothing held: the rows are zeros (the loads below need one token)
+    for (int i = threadIdx.x; i < kReadTokens * (int)per; i += kThreads) {
+      const int64_t row = t0 + i / (int)per - f, to = ((s * max_tokens + row) * c.H + h) * D + i % (int)per * 8;
+      if (row < 0 || row >= max_tokens) continue;
+      if (k_out) *reinterpret_cast<uint4 *>(k_out + to) = make_uint4(0, 0, 0, 0);
+      if (v_out) *reinterpret_cast<uint4 *>(v_out + to) = make_uint4(0, 0, 0, 0);
+    }
+    return;
+  }
+  auto page_at = [&](int64_t t) {
+    const int64_t page = pt[s * width + ((t < there ? t : there) >> lp)];
+    return (page < 0 ? 0 : page >= c.pages ? c.pages - 1 : page) * c.H + h;
+  };
+  int64_t kpage[NJ], vpage[NV];
+  int kt[NJ], vg[NV];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    kt[j] = (threadIdx.x + j * kThreads) * by_per >> 20;
+    kpage[j] = page_at(t0 + kt[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    vg[j] = (threadIdx.x + j * kThreads) * by_d >> 20;
+    vpage[j] = page_at(t0 + 16 * vg[j]);
+  }
+  uint2 k[NJ];
+  float ks[NJ], vs[NV];
+  uint4 v[NV];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int i = threadIdx.x + j * kThreads;
+    k[j] = *reinterpret_cast<const uint2 *>(c.kc + ((kpage[j] << lp) + ((t0 + kt[j]) & in_page)) * D + (i - kt[j] * (int)per) * 8);
+    ks[j] = c.ks[kpage[j]];
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int i = threadIdx.x + j * kThreads;
+    v[j] = *reinterpret_cast<const uint4 *>(c.vc + ((vpage[j] << lp) + ((t0 + 16 * vg[j]) & in_page)) * D + (i - vg[j] * D) * 16);
+    vs[j] = c.vs[vpage[j]];
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int i = threadIdx.x + j * kThreads, ch = i - vg[j] * D;
+    if (vg[j] >= kReadTokens / 16) continue;
+    *reinterpret_cast<uint4 *>(vt + vg[j] * 18 * D + (ch + ch / 8) * 16) = v[j];
+    if (ch == 0) vscale[vg[j]] = vs[j];
+  }
   __syncthreads();
-  for (int i = threadIdx.x; i < 16 * (D / 8); i += kThreads) {
-    const int t = i / (D / 8), d = i % (D / 8) * 8;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int i = threadIdx.x + j * kThreads, t = kt[j], piece = i - t * (int)per;
     const int64_t row = t0 + t - f;
-    if (row < 0 || row >= max_tokens) continue;
-    const bool on = there && t0 + t < e;
-    const int64_t at = ((s * max_tokens + row) * c.H + h) * D + d;
+    if (t >= kReadTokens || row < 0 || row >= max_tokens) continue;
+    const bool on = t0 + t <= there;
+    const int64_t to = ((s * max_tokens + row) * c.H + h) * D + piece * 8;
     float x[8];
     if (k_out) {
-      uint2 u = make_uint2(0, 0);
-      if (on) u = *reinterpret_cast<const uint2 *>(c.kc + page * P * D + (int64_t)(o + t) * D + d);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = on ? (float)(int8_t)((j < 4 ? u.x : u.y) >> (8 * (j % 4))) * ks : 0.0f;
-      *reinterpret_cast<uint4 *>(k_out + at) = pack8(x);
+      for (int b = 0; b < 8; ++b) x[b] = on ? (float)(int8_t)((b < 4 ? k[j].x : k[j].y) >> (8 * (b % 4))) * ks[j] : 0.0f;
+      *reinterpret_cast<uint4 *>(k_out + to) = pack8(x);
     }
     if (v_out) {
+      const int8_t *at = reinterpret_cast<const int8_t *>(vt + t / 16 * 18 * D + piece * 144 + t % 16);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = on ? (float)vt[(d + j) * 16 + t] * vs : 0.0f;
-      *reinterpret_cast<uint4 *>(v_out + at) = pack8(x);
+      for (int b = 0; b < 8; ++b) x[b] = on ? (float)at[16 * b] * vscale[t / 16] : 0.0f;
+      *reinterpret_cast<uint4 *>(v_out + to) = pack8(x);
     }
   }
 }
 
-// Slices of H heads for `units` tokens: up to 8 heads share a lane group's angles and weights
-// where there are groups enough to fill the card (about eight waves a SIMD).
-int slices(int64_t tokens, int heads_all, int H, int L) {
+// Heads of a token that one lane group takes in turn, with the token's angles and the weights in
+// registers: up to `most`, where there are groups enough to fill the card (eight waves a SIMD).
+int slices(int64_t tokens, int heads_all, int H, int L, int most) {
   if (H == 0) return 0;
-  int per = 8;
+  int per = most;
   while (per > 1 && tokens * ((heads_all + per - 1) / per) * L / 64 < 8192) per /= 2;
   return (H + per - 1) / per;
 }
@@ -436,7 +502,7 @@ hipError_t launch_qk_rope(const Heads &q, int Hq, const Heads &k, int Hk, const 
                           uint16_t *q_out, uint16_t *k_out, hipStream_t s) {
   return with_lanes(D, [&](auto l) {
     constexpr int L = decltype(l)::value;
-    const int Sq = slices(T, Hq + Hk, Hq, L), Sk = slices(T, Hq + Hk, Hk, L);
+    const int Sq = Hq, Sk = Hk;
     const int64_t blocks = (T * (Sq + Sk) + kThreads / L - 1) / (kThreads / L);
     qk_rope_kernel<L><<<dim3((unsigned)blocks), kThreads, 0, s>>>(q, Hq, Sq, k, Hk, Sk, r, T, D, q_out, k_out);
     return hipGetLastError();
@@ -449,20 +515,37 @@ hipError_t launch_cache_append(const Cache &c, const Batch &b, const Heads &k, c
     constexpr int L = decltype(l)::value;
     const int pages = (int)((b.max_new + 2 * c.P - 2) / c.P);  // pages that max_new tokens can reach
     const int64_t kv_items = b.seqs * pages * c.H * 2;
-    const int Sq = slices(b.seqs * b.max_new, Hq, Hq, L);
+    const int Sq = slices(b.seqs * b.max_new, Hq, Hq, L, 8);
     const int64_t q_blocks = Hq ? (b.max_new * Sq + kThreads / L - 1) / (kThreads / L) : 0;
-    cache_append_kernel<L><<<dim3((unsigned)(kv_items + b.seqs * q_blocks)), kThreads, c.P * c.D, s>>>(
-        c, b, k, v, q, Hq, Sq, kv_items, pages, q_blocks, r, T, q_out);
-    return hipGetLastError();
+    const unsigned blocks = (unsigned)(kv_items + b.seqs * q_blocks);
+    const size_t lds = (size_t)c.P * c.D / 16 * 17;
+    const int64_t tokens = b.max_new < c.P ? b.max_new : c.P;  // of a page
+    auto go = [&](auto np) {
+      cache_append_kernel<L, decltype(np)::value><<<dim3(blocks), kThreads, lds, s>>>(c, b, k, v, q, Hq, Sq, kv_items, pages,
+                                                                                   q_blocks, r, T, q_out);
+      return hipGetLastError();
+    };
+    const int64_t passes = (tokens + kThreads / L - 1) / (kThreads / L);
+    if (passes <= 1) return go(std::integral_constant<int, 1>{});
+    if (passes <= 2) return go(std::integral_constant<int, 2>{});
+    if (passes <= 4) return go(std::integral_constant<int, 4>{});
+    return go(std::integral_constant<int, 8>{});
   });
 }
 
 hipError_t launch_cache_read(const Cache &c, const int32_t *pt, int64_t width, const int32_t *first,
                              const int32_t *last, int64_t seqs, int64_t max_tokens, uint16_t *k_out, uint16_t *v_out,
                              hipStream_t s) {
-  const int groups = (int)((max_tokens + 15) / 16 + 1);
-  cache_read_kernel<<<dim3((unsigned)(seqs * groups * c.H)), kThreads, 0, s>>>(c, pt, width, first, last, groups,
-                                                                              max_tokens, k_out, v_out);
+  const int windows = (int)((max_tokens + 15 + kReadTokens - 1) / kReadTokens);
+  const dim3 grid((unsigned)(seqs * windows * c.H));
+  if (c.D <= 32)
+    cache_read_kernel<1><<<grid, kThreads, 0, s>>>(c, pt, width, first, last, windows, max_tokens, k_out, v_out);
+  else if (c.D <= 64)
+    cache_read_kernel<2><<<grid, kThreads, 0, s>>>(c, pt, width, first, last, windows, max_tokens, k_out, v_out);
+  else if (c.D <= 128)
+    cache_read_kernel<4><<<grid, kThreads, 0, s>>>(c, pt, width, first, last, windows, max_tokens, k_out, v_out);
+  else
+    cache_read_kernel<8><<<grid, kThreads, 0, s>>>(c, pt, width, first, last, windows, max_tokens, k_out, v_out);
   return hipGetLastError();
 }
 

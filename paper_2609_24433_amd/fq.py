@@ -431,64 +431,76 @@ def kv_cache(pages: int, heads: int, page_tokens: int, head_dim: int, device="cu
                    torch.zeros((pages, heads), dtype=torch.float32, device=device))
 
 
-def _ptr0(t: Optional[torch.Tensor]) -> int:
-    return 0 if t is None else t.data_ptr()
+# A decoding step's calls are bound by the host: these helpers build no message unless a check
+# fails and read each property of a tensor once.
+
+_BF16, _F32, _I32, _I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
 
 
 def _heads(x: torch.Tensor, name: str) -> bytes:
-    _require(x.dtype == torch.bfloat16 and x.stride(-1) == 1, f"{name}: bf16 with unit stride of the last dim")
     s = x.stride()
+    if x.dtype is not _BF16 or s[-1] != 1:
+        raise ValueError(f"{name}: bf16 with unit stride of the last dim")
     return _HEADS(x.data_ptr(), s[0] if len(s) == 4 else 0, s[-3], s[-2])
 
 
 def _index(t: Optional[torch.Tensor], n: int, name: str) -> int:
     if t is None:
         return 0
-    _require(t.dtype == torch.int32 and t.dim() == 1 and t.shape[0] == n and (n < 2 or t.stride(0) == 1),
-             f"{name}: contiguous int32 [{n}]")
+    if t.dtype is not _I32 or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name}: contiguous int32 [{n}]")
     return t.data_ptr()
 
 
-def _cache_desc(c: KVCache) -> Tuple[bytes, int, int]:
+def _weight(w: Optional[torch.Tensor], D: int, name: str) -> int:
+    if w is None:
+        return 0
+    if w.dtype is not _F32 or w.shape != (D,) or w.stride(0) != 1:
+        raise ValueError(f"{name}: contiguous fp32 [{D}]")
+    return w.data_ptr()
+
+
+def _cache_desc(c: KVCache) -> Tuple[bytes, int, int, int]:
     kc, ks, vc, vs = c
     pages, H, P, D = kc.shape
-    _require(kc.dtype == torch.int8 and vc.dtype == torch.int8 and tuple(vc.shape) == (pages, H, P // 16, D, 16)
-             and kc.is_contiguous() and vc.is_contiguous(), "cache codes: contiguous int8 [pages, heads, P, D] and [pages, heads, P/16, D, 16]")
-    _require(ks.dtype == torch.float32 and vs.dtype == torch.float32 and tuple(ks.shape) == (pages, H)
-             and tuple(vs.shape) == (pages, H) and ks.is_contiguous() and vs.is_contiguous(),
-             "cache scales: contiguous fp32 [pages, heads]")
-    return _CACHE(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), pages, H, P, D, 0), H, D
+    if (kc.dtype is not _I8 or vc.dtype is not _I8 or vc.shape != (pages, H, P // 16, D, 16) or not kc.is_contiguous()
+            or not vc.is_contiguous()):
+        raise ValueError("cache codes: contiguous int8 [pages, heads, P, D] and [pages, heads, P/16, D, 16]")
+    if (ks.dtype is not _F32 or vs.dtype is not _F32 or ks.shape != (pages, H) or vs.shape != (pages, H)
+            or not ks.is_contiguous() or not vs.is_contiguous()):
+        raise ValueError("cache scales: contiguous fp32 [pages, heads]")
+    return _CACHE(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), pages, H, P, D, 0), H, P, D
 
 
-def _batch_desc(page_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, max_new: int, max_kv: int = 0,
-                page_tokens: int = 0) -> bytes:
-    """fq_kv_batch; page_tokens instead of max_kv: all tokens that the table holds."""
-    _require(page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous(),
-             "page_table: contiguous int32 [seqs, pages]")
-    B, width = page_table.shape
-    return _BATCH(_index(q_start, B + 1, "q_start"), _index(kv_len, B, "kv_len"), page_table.data_ptr(), width, B, max_new,
-                  max_kv or width * page_tokens)
+def _table_shape(page_table: torch.Tensor) -> Tuple[int, int]:
+    shape = page_table.shape
+    if page_table.dtype is not _I32 or len(shape) != 2 or not page_table.is_contiguous():
+        raise ValueError("page_table: contiguous int32 [seqs, pages]")
+    return shape
+
+
+def _batch_desc(page_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, max_new: int, max_kv: int) -> bytes:
+    B, width = _table_shape(page_table)
+    return _BATCH(_index(q_start, B + 1, "q_start"), _index(kv_len, B, "kv_len"), page_table.data_ptr(), width, B, max_new, max_kv)
 
 
 def _rope_desc(table, positions, T, q_weight, k_weight, D, eps, interleaved) -> bytes:
-    length = rot = 0
+    length = pairs = at = 0
     if table is not None:
-        _require(table.dtype == torch.float32 and table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous(),
-                 "table: contiguous fp32 [length, R/2, 2]")
-        length, rot = table.shape[0], 2 * table.shape[1]
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        _require(w is None or (w.dtype == torch.float32 and tuple(w.shape) == (D,) and w.is_contiguous()),
-                 f"{name}: contiguous fp32 [{D}]")
-    return _ROPE(_ptr0(table), length, _index(positions, T, "positions"), _ptr0(q_weight), _ptr0(k_weight), eps, rot,
-                 int(interleaved), 0)
+        shape = table.shape
+        if table.dtype is not _F32 or len(shape) != 3 or shape[2] != 2 or not table.is_contiguous():
+            raise ValueError("table: contiguous fp32 [length, R/2, 2]")
+        length, pairs, at = shape[0], shape[1], table.data_ptr()
+    return _ROPE(at, length, _index(positions, T, "positions"), _weight(q_weight, D, "q_weight"),
+                 _weight(k_weight, D, "k_weight"), eps, 2 * pairs, interleaved, 0)
 
 
-def _check_rows(out: Optional[torch.Tensor], like: torch.Tensor, name: str) -> torch.Tensor:
-    """A contiguous bf16 output of the shape of `like`, the caller's or a new one."""
+def _rows(out: Optional[torch.Tensor], like: torch.Tensor, shape: Tuple[int, ...], name: str) -> torch.Tensor:
+    """A contiguous bf16 output, the caller's or a new one on the device of `like` (bf16)."""
     if out is None:
-        return torch.empty(like.shape, dtype=torch.bfloat16, device=like.device)
-    _require(out.dtype == torch.bfloat16 and out.shape == like.shape and out.is_contiguous(),
-             f"{name}: contiguous bf16 {tuple(like.shape)}")
+        return like.new_empty(shape) if type(like) is torch.Tensor else torch.empty(shape, dtype=_BF16, device=like.device)
+    if out.dtype is not _BF16 or out.shape != shape or not out.is_contiguous():
+        raise ValueError(f"{name}: contiguous bf16 {tuple(shape)}")
     return out
 
 
@@ -531,16 +543,20 @@ def qk_rope(q: torch.Tensor, k: Optional[torch.Tensor], table: Optional[torch.Te
     """Norms of queries and keys per head (where a weight fp32 [D] is given) and the rotation of their first
     2 * table.shape[1] dims, halves or (interleaved) adjacent pairs: bf16 q [T, Hq, D], k [T, Hk, D], any strides of
     multiples of 8 -> contiguous (q_out, k_out).  positions int32 [T] (None: 0, 1, ...)."""
-    T, Hq, D = q.shape
-    Hk = 0
-    if k is not None:
-        Hk = k.shape[1]
-        _require(tuple(k.shape) == (T, Hk, D), "k: [T, Hk, D] of q's T and D")
+    shape = q.shape
+    T, Hq, D = shape
     rope = _rope_desc(table, positions, T, q_weight, k_weight, D, eps, interleaved)
-    yq = _check_rows(q_out, q, "q_out")
-    yk = None if k is None else _check_rows(k_out, k, "k_out")
-    _check(LIB.fq_qk_rope(_heads(q, "q"), Hq, None if k is None else _heads(k, "k"), Hk, rope, T, D, yq.data_ptr(),
-                          _ptr(yk), _stream_handle()))
+    hq, hk, Hk, yk = _heads(q, "q"), None, 0, None
+    yq = _rows(q_out, q, shape, "q_out")
+    if k is not None:
+        shape = k.shape
+        Hk = shape[1]
+        if shape != (T, Hk, D):
+            raise ValueError("k: [T, Hk, D] of q's T and D")
+        hk, yk = _heads(k, "k"), _rows(k_out, k, shape, "k_out")
+    rc = LIB.fq_qk_rope(hq, Hq, hk, Hk, rope, T, D, yq.data_ptr(), None if yk is None else yk.data_ptr(), _stream_handle())
+    if rc:
+        _check(rc)
     return yq, yk
 
 
@@ -553,36 +569,44 @@ def cache_append(cache: KVCache, page_table: torch.Tensor, q_start: torch.Tensor
     the kv_len[b] tokens of sequence b) to its pages: keys normed and rotated as by qk_rope, keys and values rounded to 8
     bits under a scale per page and head.  q [T, Hq, D] is normed and rotated in the same launch and returned.
     max_new: the most rows of a sequence.  positions: None for a token's place in its sequence."""
-    T, H, D = k.shape
-    desc, ch, cd = _cache_desc(cache)
-    _require(H == ch and D == cd and tuple(v.shape) == (T, H, D), "k, v: [T, heads, D] of the cache's heads and D")
-    batch = _batch_desc(page_table, q_start, kv_len, max_new, page_tokens=cache.k_codes.shape[2])
+    shape = k.shape
+    T, H, D = shape
+    desc, ch, P, cd = _cache_desc(cache)
+    if H != ch or D != cd or v.shape != shape:
+        raise ValueError("k, v: [T, heads, D] of the cache's heads and D")
+    batch = _batch_desc(page_table, q_start, kv_len, max_new, page_table.shape[1] * P if page_table.dim() == 2 else 0)
     y, Hq, hq = None, 0, None
     if q is not None:
-        Hq = q.shape[1]
-        _require(tuple(q.shape) == (T, Hq, D), "q: [T, Hq, D] of k's T and D")
-        y, hq = _check_rows(q_out, q, "q_out"), _heads(q, "q")
+        shape = q.shape
+        Hq = shape[1]
+        if shape != (T, Hq, D):
+            raise ValueError("q: [T, Hq, D] of k's T and D")
+        hq, y = _heads(q, "q"), _rows(q_out, q, shape, "q_out")
     rope = _rope_desc(table, positions, T, q_weight, k_weight, D, eps, interleaved)
-    _check(LIB.fq_cache_append(desc, batch, _heads(k, "k"), _heads(v, "v"), hq, Hq, rope, T, _ptr(y), _stream_handle()))
+    rc = LIB.fq_cache_append(desc, batch, _heads(k, "k"), _heads(v, "v"), hq, Hq, rope, T, None if y is None else y.data_ptr(),
+                             _stream_handle())
+    if rc:
+        _check(rc)
     return y
 
 
 def cache_read(cache: KVCache, page_table: torch.Tensor, first: torch.Tensor, last: torch.Tensor, max_tokens: int,
                k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Tokens first[b] .. last[b] - 1 of every sequence as values: bf16 k, v [seqs, max_tokens, heads, D], zeros beyond."""
-    desc, H, D = _cache_desc(cache)
-    _require(page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous(),
-             "page_table: contiguous int32 [seqs, pages]")
-    B, width = page_table.shape
+    desc, H, _, D = _cache_desc(cache)
+    B, width = _table_shape(page_table)
     shape = (B, max_tokens, H, D)
+    if k_out is None or v_out is None:
+        new = torch.empty((2, *shape), dtype=_BF16, device=page_table.device)
+        k_out, v_out = new[0] if k_out is None else k_out, new[1] if v_out is None else v_out
     for o, name in ((k_out, "k_out"), (v_out, "v_out")):
-        _require(o is None or (o.dtype == torch.bfloat16 and tuple(o.shape) == shape and o.is_contiguous()),
-                 f"{name}: contiguous bf16 {shape}")
-    k = torch.empty(shape, dtype=torch.bfloat16, device=page_table.device) if k_out is None else k_out
-    v = torch.empty(shape, dtype=torch.bfloat16, device=page_table.device) if v_out is None else v_out
-    _check(LIB.fq_cache_read(desc, page_table.data_ptr(), width, _index(first, B, "first"), _index(last, B, "last"), B,
-                             max_tokens, k.data_ptr(), v.data_ptr(), _stream_handle()))
-    return k, v
+        if o.dtype is not _BF16 or o.shape != shape or not o.is_contiguous():
+            raise ValueError(f"{name}: contiguous bf16 {shape}")
+    rc = LIB.fq_cache_read(desc, page_table.data_ptr(), width, _index(first, B, "first"), _index(last, B, "last"), B, max_tokens,
+                           k_out.data_ptr(), v_out.data_ptr(), _stream_handle())
+    if rc:
+        _check(rc)
+    return k_out, v_out
 
 
 def cache_attention_workspace_bytes(T: int, Hq: int, Hk: int, D: int, seqs: int, max_new: int, max_kv: int) -> int:
@@ -595,15 +619,19 @@ def cache_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, q
     """softmax(scale q k^T) v of a ragged batch of queries bf16 [T, Hq, D] over its sequences' tokens in the cache (see
     cache_append; append first) -> [T, Hq, D].  max_new, max_kv: the most rows and tokens of a sequence; scale: None for
     1/sqrt(D); causal: a row sees the tokens up to its own place, otherwise all kv_len[b]."""
-    T, Hq, D = q.shape
-    desc, H, cd = _cache_desc(cache)
-    _require(D == cd, "q: [T, Hq, D] of the cache's D")
+    shape = q.shape
+    T, Hq, D = shape
+    desc, H, _, cd = _cache_desc(cache)
+    if D != cd:
+        raise ValueError("q: [T, Hq, D] of the cache's D")
     batch = _batch_desc(page_table, q_start, kv_len, max_new, max_kv)
-    y = _check_rows(out, q, "out")
+    hq, y = _heads(q, "q"), _rows(out, q, shape, "out")
     if ws is None:
         ws = _scratch(LIB.fq_cache_attention_workspace_bytes(T, Hq, H, D, page_table.shape[0], max_new, max_kv), q.device)
-    _check(LIB.fq_cache_attention(_heads(q, "q"), Hq, T, desc, batch, D ** -0.5 if scale is None else scale, int(causal),
-                                  y.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(), _stream_handle()))
+    rc = LIB.fq_cache_attention(hq, Hq, T, desc, batch, D ** -0.5 if scale is None else scale, causal, y.data_ptr(),
+                                None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream_handle())
+    if rc:
+        _check(rc)
     return y
 
 
@@ -617,18 +645,23 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kv_len: O
     """softmax(scale q k^T) v of queries bf16 [B, Sq, Hq, D] over an encoder's states k, v [B, Sk, Hk, D] (any strides of
     multiples of 8) -> [B, Sq, Hq, D].  kv_len int32 [B]: states in use; key_mask bool [B, Sk]: True = seen.  What lies in
     unseen places has no effect; a sample that sees nothing gives zeros."""
-    B, Sq, Hq, D = q.shape
-    Sk, Hk = k.shape[1], k.shape[2]
-    _require(tuple(k.shape) == (B, Sk, Hk, D) and v.shape == k.shape, "k, v: [B, Sk, Hk, D] of q's B and D")
-    stride = 0
+    shape, ks = q.shape, k.shape
+    B, Sq, Hq, D = shape
+    _, Sk, Hk, _ = ks
+    if ks != (B, Sk, Hk, D) or v.shape != ks:
+        raise ValueError("k, v: [B, Sk, Hk, D] of q's B and D")
+    mask = stride = 0
     if key_mask is not None:
-        _require(key_mask.dtype in (torch.bool, torch.uint8) and tuple(key_mask.shape) == (B, Sk)
-                 and (Sk < 2 or key_mask.stride(1) == 1), "key_mask: bool [B, Sk] with unit stride of the last dim")
-        stride = key_mask.stride(0)
-    y = _check_rows(out, q, "out")
+        if (key_mask.dtype not in (torch.bool, torch.uint8) or key_mask.shape != (B, Sk)
+                or (Sk > 1 and key_mask.stride(1) != 1)):
+            raise ValueError("key_mask: bool [B, Sk] with unit stride of the last dim")
+        mask, stride = key_mask.data_ptr(), key_mask.stride(0)
+    hq, y = _heads(q, "q"), _rows(out, q, shape, "out")
     if ws is None:
         ws = _scratch(LIB.fq_cross_attention_workspace_bytes(B, Sq, Sk, Hq, Hk, D), q.device)
-    _check(LIB.fq_cross_attention(_heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _index(kv_len, B, "kv_len") or None,
-                                  _ptr(key_mask), stride, B, Sq, Sk, Hq, Hk, D, D ** -0.5 if scale is None else scale,
-                                  y.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(), _stream_handle()))
+    rc = LIB.fq_cross_attention(hq, _heads(k, "k"), _heads(v, "v"), _index(kv_len, B, "kv_len") or None, mask or None, stride, B, Sq,
+                                Sk, Hq, Hk, D, D ** -0.5 if scale is None else scale, y.data_ptr(),
+                                None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream_handle())
+    if rc:
+        _check(rc)
     return y
