@@ -5,8 +5,11 @@
 namespace fq {
 namespace {
 
-// Rows of one key head up to which the keys are streamed for 16 rows at a time.
-constexpr int kStreamRows = 16;
+// Rows of one key head up to which the keys are streamed for 16 rows at a time, every 16 reading
+// them again (from the caches).  8 sequences of up to 8192 tokens in the cache, 8 key heads of 128:
+// 32 rows take 26 us (tiles 50), 48 rows 29 (49), 64 rows 42 (52).  8 samples of 4000 states, 16 heads
+// of 128: 32 rows 95 us (tiles 96), 50 rows 141 (97).
+constexpr int kStreamRowsCached = 64, kStreamRowsStates = 32;
 
 struct Plan {
   int rows;   // of a workgroup: 16 streaming, 128 or 256 with tiles
@@ -16,12 +19,12 @@ struct Plan {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Streaming: parts of 256 tokens of a cache or 128 states (the same bytes at two a value), so that
-// waves of ragged sequences end evenly: 64 sequences of up to 8192 tokens take 82 us with parts of
-// 256, 94 with 512, 105 with 1024; parts under that pay their start-up (131 with 128 workgroups'
-// worth).  Parts get longer where there would be more than 32768 of them (their results cost room
-// and time) and shorter, down to a tile, where there are too few to fill the card: one sequence of
-// 877 tokens takes 13 us with 64, 19 with 128, 28 with 256.
+// Streaming: parts of 64 KB of keys and values (256 cached tokens of head 128), so that waves of
+// ragged sequences end evenly: 64 sequences of up to 8192 tokens, head 128, take 80 us, with 32 KB 85
+// and with 128 KB 81; 32 of up to 4096, head 256, take 30, 33 and 37.  Parts get longer where there
+// would be more than 32768 of them (their results cost room and time) and shorter, down to a tile,
+// where there are too few to fill the card: one sequence of 877 tokens, head 256, takes 10 us with 64
+// tokens a part, 19 with 128, 28 with 256.
 // Tiles: 256 rows a workgroup of eight waves where there are more than 128 rows and the head size
 // leaves the registers (head 128, 4096 rows over 8190 tokens: 414 us, with 128 rows 444), one a
 // compute unit; two of 128 rows fit otherwise.  Tokens are split only to fill the card, 128 or more
@@ -29,16 +32,15 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 Plan plan_attention(bool cached, int Hq, int Hk, int D, int64_t seqs, int64_t max_new, int64_t max_kv) {
   Plan p;
   const int64_t rows = max_new * (Hq / Hk);
-  const bool stream = rows <= kStreamRows;
+  const bool stream = rows <= (cached ? kStreamRowsCached : kStreamRowsStates);
   p.rows = stream ? 16 : rows > 128 && D > 64 && D <= 128 ? 256 : 128;
   const int64_t groups = seqs * Hk * ceil_div(rows, p.rows);
   int64_t chunk;
   if (stream) {
     chunk = ceil_div(ceil_div(max_kv * groups, 32768), 64) * 64;
-    const int64_t least = cached ? 256 : 128;
+    const int64_t least = 65536 / ((cached ? 2 : 4) * D) / 64 * 64;
     if (chunk < least) chunk = least;
-    while (chunk > 64 && groups * ceil_div(max_kv, chunk) < 1024) chunk /= 2;
-    chunk = ceil_div(chunk, 64) * 64;
+    while (chunk > 64 && groups * ceil_div(max_kv, chunk) < 1024) chunk = ceil_div(chunk / 2, 64) * 64;
   } else {
     const int64_t want = p.rows == 256 ? 256 : 512, splits = groups >= want ? 1 : want / groups;
     chunk = ceil_div(ceil_div(max_kv, splits), 128) * 128;

@@ -374,6 +374,9 @@ __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_k
     }
     if (n > 0) {
       const int k = n - 1, x = k / 4 % RT, y = k / (4 * RT) * 4 + k % 4;
+      // Weights enter the product as bf16, with the scale of the values in them: 9 bits of each, as the
+      // result will have.  What the rounding drops would take a second product, and matrix instructions
+      // bound the kernel.
       uint32_t u;
       if constexpr (CACHED) {
         l[x][0] += p0;
