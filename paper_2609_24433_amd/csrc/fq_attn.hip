@@ -11,6 +11,13 @@ namespace {
 // of 128: 32 rows 95 us (tiles 96), 50 rows 141 (97).
 constexpr int kStreamRowsCached = 64, kStreamRowsStates = 32;
 
+// Streaming waves of 64 tokens up to which calls with more rows stream too: the card has a place for
+// each, and a tile's walk would take longer than all of them (head above 128: half as many fit).  One
+// sequence of 866 tokens, 8 query heads on one of 256: 50 rows of tokens, 350 waves, 14 us (tiles 20),
+// 100, 700 waves, 21 (21); 4 key heads of 64, 200 rows each: 728 waves, 9.8 us (12.0).  50 queries
+// against 816 states, 16 heads on 8 of 128: 728 waves, 11 us (17).
+constexpr int kStreamWaves = 1024;
+
 struct Plan {
   int rows;   // of a workgroup: 16 streaming, 128 or 256 with tiles
   int chunk;  // tokens of a part
@@ -32,7 +39,8 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 Plan plan_attention(bool cached, int Hq, int Hk, int D, int64_t seqs, int64_t max_new, int64_t max_kv) {
   Plan p;
   const int64_t rows = max_new * (Hq / Hk);
-  const bool stream = rows <= (cached ? kStreamRowsCached : kStreamRowsStates);
+  const double waves = (double)(seqs * Hk) * ceil_div(rows, 16) * ceil_div(max_kv, 64);
+  const bool stream = rows <= (cached ? kStreamRowsCached : kStreamRowsStates) || waves <= (D > 128 ? kStreamWaves / 2 : kStreamWaves);
   p.rows = stream ? 16 : rows > 128 && D > 64 && D <= 128 ? 256 : 128;
   const int64_t groups = seqs * Hk * ceil_div(rows, p.rows);
   int64_t chunk;
