@@ -280,7 +280,7 @@ fq_status fq_gptq_sweep(const float *w_t, int64_t ldw, const double *U, int64_t 
 
 /* bf16 rows of heads: element d of head h of token t (of sequence b) at
  * p[b batch_stride + t token_stride + h head_stride + d], strides in elements, multiples of
- * 8 and at least 0 (a stride is not looked at where its count is 1). */
+ * 8 and at least 0, token_stride up to 2^24 (a stride is not looked at where its count is 1). */
 typedef struct {
   const void *p;
   int64_t batch_stride, token_stride, head_stride;

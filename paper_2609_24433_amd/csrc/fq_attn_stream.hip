@@ -9,9 +9,9 @@
 //
 // Bound by memory where there are many sequences, by the latency of a wave's walk and of the join's
 // launch where there are few.  Measured, with the join: 64 sequences of up to 8192 tokens in the
-// cache, 8 key heads of 128, 32 query heads: 80 us, 4.1 TB/s; two of 131071 tokens, 2 key heads, 37 us,
-// 3.6 TB/s; one of 877 tokens, one key head of 256, 10 us; a query in each of 24 samples of up to 1500
-// bf16 states, 16 heads of 128: 38 us, 4.3 TB/s.
+// cache, 8 key heads of 128, 32 query heads: 80 us, 4.1 TB/s; two of 131071 tokens, 2 key heads, 33 us,
+// 4.0 TB/s; one of 877 tokens, one key head of 256, 10 us, and 50 tokens of one of 866 14 us; a query in
+// each of 24 samples of up to 1500 bf16 states, 16 heads of 128: 38 us, 4.3 TB/s.
 #include "fq_attn_device.hpp"
 #include "fq_attn_launch.hpp"
 

@@ -9,6 +9,11 @@
 //   V^T P^T of u       with  the last weights of u, the maxima of u + 1 and the staging of a tile's
 //                            values (first half: of the next tile) or keys (second: the one after)
 // Loads run a tile ahead of the staging.
+//
+// Measured, with the join: 4096 tokens over 8190 in the cache, causal, 32 query heads on 8 of 128: 411
+// us, 1.00 PFLOP/s, 0.8 of what a plain product of 8192^3 reaches (the pipeline alone, its operands
+// left in LDS, 358 us); 4 samples of 1031 queries over up to 4099 masked bf16 states, 16 heads on 8 of
+// 128: 149 us (94 alone: the longest sample's workgroups run with part of the card idle).
 #include "fq_attn_device.hpp"
 #include "fq_attn_launch.hpp"
 

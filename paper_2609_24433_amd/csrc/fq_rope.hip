@@ -3,7 +3,15 @@
 // A head of D values is held by D/16 lanes of a group of L (the next power of two), 16 values a
 // lane: the two 8-value chunks that the rotation pairs, dims [8m, 8m + 8) and the same R/2
 // further on (halves), or 16 adjacent dims (adjacent pairs, and dims the rotation leaves alone).
-// So a rotation never crosses lanes, and the only exchange is the norm's sum.
+// So a rotation never crosses lanes, and the only exchange is the norm's sum.  Norm and rotation are
+// fp32 from the bf16 input to the one rounding at the end.
+//
+// All are bound by memory where they are long and by launches and the latency of dependent loads
+// where they are short.  Measured: norm and rotation of 16385 tokens, 40 heads of 128: 78 us, 4.4 TB/s; of
+// 50 tokens, 9 heads of 256: 4.1 us.  Append of a prompt of 16383 tokens, 32 query and 8 key heads of
+// 128: 94 us, 4.4 TB/s; of one token to each of 32 sequences: 6 us, of which most is a page's chain of
+// waits (lengths, table entry, scale, codes).  Read of the last page of each
+// of 32 sequences: 8 us; of 16383 tokens, 8 heads of 128: 23 us, 4.3 TB/s.
 #include <cfloat>
 
 #include "fq_attn.hpp"
