@@ -326,7 +326,8 @@ typedef struct {
  *               sequence's last n tokens are its rows of this call)
  *   page_table  [seqs, table_width]: page of tokens P w .. P w + P - 1 of the sequence
  * max_new and max_kv are bounds of the rows of a sequence and of kv_len, known to the host;
- * rows and tokens beyond them are not computed or seen.  table_width * P >= max_kv.  An
+ * rows and tokens beyond them are not computed or seen (the first max_new rows of a longer sequence keep
+ * the places that q_start and kv_len give them).  table_width * P >= max_kv.  An
  * entry outside the pool is clamped into it.  Pages in use by two sequences may be read, not appended to. */
 typedef struct {
   const int32_t *q_start, *kv_len, *page_table;
@@ -346,7 +347,8 @@ fq_status fq_qk_rope(const fq_heads *q, int Hq, const fq_heads *k, int Hk, const
                      void *q_out, void *k_out, void *stream);
 
 /* Appends T tokens (all sequences of the batch) to the cache: token i of sequence b goes to
- * slot kv_len[b] - n_b + i, its keys normed and rotated, its values as they are.  For every
+ * slot kv_len[b] - n_b + i (n_b = q_start[b+1] - q_start[b]; a row whose slot is negative is dropped), its
+ * keys normed and rotated, its values as they are.  For every
  * page and head that new tokens reach, with a = max |x| over them in fp32:
  *   scale' = a / 127, or max(scale, a / 127) where the page holds earlier tokens;
  *   earlier codes = rne(code * (scale / scale')) where the scale grew;

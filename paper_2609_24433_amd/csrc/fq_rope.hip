@@ -170,12 +170,13 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(Heads q, int Hq, int 
 
 // ---------------------------------------------------------------- appends
 
-// The rows of sequence s in this call: [row, row + n), and the slot of its first token (which may
-// be negative where kv_len is short: those tokens are dropped).
+// The rows of sequence s that this call computes: [row, row + n), and their slots [begin, end).  All the
+// sequence's rows count for the slot of the first one, those past max_new too: row i goes to slot kv_len - rows + i
+// (which is negative where kv_len is short: such rows are dropped).
 struct Span1 {
   int64_t row;
   int n;
-  int64_t begin, end;  // slots
+  int64_t begin, end;
 };
 __device__ __forceinline__ Span1 sequence_rows(const Batch &b, int64_t s, int64_t T) {
   Span1 r;
@@ -186,8 +187,8 @@ __device__ __forceinline__ Span1 sequence_rows(const Batch &b, int64_t s, int64_
   const int64_t m = b.kv_len[s];
   r.row = q0;
   r.n = (int)n;
-  r.begin = m - n;
-  r.end = m < b.max_kv ? m : b.max_kv;
+  r.begin = m - (q1 - q0);
+  r.end = r.begin + n < b.max_kv ? r.begin + n : b.max_kv;
   return r;
 }
 
