@@ -17,9 +17,9 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfq.so")
 
-FQ_OK = 0
+FQ_OK, FQ_ERR_ALIAS = 0, 7
 _STATUS = {1: "FQ_ERR_NULL", 2: "FQ_ERR_SHAPE", 3: "FQ_ERR_UNSUPPORTED", 4: "FQ_ERR_ALIGN",
-           5: "FQ_ERR_WORKSPACE", 6: "FQ_ERR_HIP", 7: "FQ_ERR_ALIAS"}
+           5: "FQ_ERR_WORKSPACE", 6: "FQ_ERR_HIP", FQ_ERR_ALIAS: "FQ_ERR_ALIAS"}
 
 EXPORTED = ["fq_fwht_quant", "fq_quantize_weights", "fq_packed_weight_bytes", "fq_pack_weights",
             "fq_unpack_weights", "fq_gemm_workspace_bytes", "fq_gemm_w4a4", "fq_gemm_w8a8",
@@ -432,35 +432,54 @@ def kv_cache(pages: int, heads: int, page_tokens: int, head_dim: int, device="cu
 
 
 # A decoding step's calls are bound by the host: these helpers build no message unless a check
-# fails and read each property of a tensor once.
+# fails and read each property of a tensor once.  `dev` is the device of the call's first tensor (Tensor.get_device():
+# -1 is the host): every other tensor's address is only good for a kernel on the same one.
 
 _BF16, _F32, _I32, _I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
 
 
-def _heads(x: torch.Tensor, name: str) -> bytes:
+def _elsewhere(name: str, t: torch.Tensor, dev: int) -> ValueError:
+    return ValueError(f"{name} is on {t.device}, the call's first tensor on {'the host' if dev < 0 else f'GPU {dev}'}")
+
+
+def _refuse(rc: int, dev: int) -> None:
+    """A failed call.  Where the tensors are on the host, the caller gave the library an output that overlaps an input: its
+    other checks come first, with their errors, and nothing is launched on addresses that a kernel must not see."""
+    if dev < 0 and rc == FQ_ERR_ALIAS:
+        raise ValueError("the tensors are on the host, not on a GPU")
+    _check(rc)
+
+
+def _heads(x: torch.Tensor, name: str, dev: int) -> bytes:
     s = x.stride()
     if x.dtype is not _BF16 or s[-1] != 1:
         raise ValueError(f"{name}: bf16 with unit stride of the last dim")
+    if x.get_device() != dev:
+        raise _elsewhere(name, x, dev)
     return _HEADS(x.data_ptr(), s[0] if len(s) == 4 else 0, s[-3], s[-2])
 
 
-def _index(t: Optional[torch.Tensor], n: int, name: str) -> int:
+def _index(t: Optional[torch.Tensor], n: int, name: str, dev: int) -> int:
     if t is None:
         return 0
     if t.dtype is not _I32 or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{name}: contiguous int32 [{n}]")
+    if t.get_device() != dev:
+        raise _elsewhere(name, t, dev)
     return t.data_ptr()
 
 
-def _weight(w: Optional[torch.Tensor], D: int, name: str) -> int:
+def _weight(w: Optional[torch.Tensor], D: int, name: str, dev: int) -> int:
     if w is None:
         return 0
     if w.dtype is not _F32 or w.shape != (D,) or w.stride(0) != 1:
         raise ValueError(f"{name}: contiguous fp32 [{D}]")
+    if w.get_device() != dev:
+        raise _elsewhere(name, w, dev)
     return w.data_ptr()
 
 
-def _cache_desc(c: KVCache) -> Tuple[bytes, int, int, int]:
+def _cache_desc(c: KVCache, dev: int) -> Tuple[bytes, int, int, int]:
     kc, ks, vc, vs = c
     pages, H, P, D = kc.shape
     if (kc.dtype is not _I8 or vc.dtype is not _I8 or vc.shape != (pages, H, P // 16, D, 16) or not kc.is_contiguous()
@@ -469,39 +488,58 @@ def _cache_desc(c: KVCache) -> Tuple[bytes, int, int, int]:
     if (ks.dtype is not _F32 or vs.dtype is not _F32 or ks.shape != (pages, H) or vs.shape != (pages, H)
             or not ks.is_contiguous() or not vs.is_contiguous()):
         raise ValueError("cache scales: contiguous fp32 [pages, heads]")
+    for t in c:
+        if t.get_device() != dev:
+            raise _elsewhere("the cache", t, dev)
     return _CACHE(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), pages, H, P, D, 0), H, P, D
 
 
-def _table_shape(page_table: torch.Tensor) -> Tuple[int, int]:
+def _table_shape(page_table: torch.Tensor, dev: int) -> Tuple[int, int]:
     shape = page_table.shape
     if page_table.dtype is not _I32 or len(shape) != 2 or not page_table.is_contiguous():
         raise ValueError("page_table: contiguous int32 [seqs, pages]")
+    if page_table.get_device() != dev:
+        raise _elsewhere("page_table", page_table, dev)
     return shape
 
 
-def _batch_desc(page_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, max_new: int, max_kv: int) -> bytes:
-    B, width = _table_shape(page_table)
-    return _BATCH(_index(q_start, B + 1, "q_start"), _index(kv_len, B, "kv_len"), page_table.data_ptr(), width, B, max_new, max_kv)
+def _batch_desc(page_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, max_new: int, max_kv: int, dev: int) -> bytes:
+    B, width = _table_shape(page_table, dev)
+    return _BATCH(_index(q_start, B + 1, "q_start", dev), _index(kv_len, B, "kv_len", dev), page_table.data_ptr(), width, B, max_new,
+                  max_kv)
 
 
-def _rope_desc(table, positions, T, q_weight, k_weight, D, eps, interleaved) -> bytes:
+def _rope_desc(table, positions, T, q_weight, k_weight, D, eps, interleaved, dev) -> bytes:
     length = pairs = at = 0
     if table is not None:
         shape = table.shape
         if table.dtype is not _F32 or len(shape) != 3 or shape[2] != 2 or not table.is_contiguous():
             raise ValueError("table: contiguous fp32 [length, R/2, 2]")
+        if table.get_device() != dev:
+            raise _elsewhere("table", table, dev)
         length, pairs, at = shape[0], shape[1], table.data_ptr()
-    return _ROPE(at, length, _index(positions, T, "positions"), _weight(q_weight, D, "q_weight"),
-                 _weight(k_weight, D, "k_weight"), eps, 2 * pairs, interleaved, 0)
+    return _ROPE(at, length, _index(positions, T, "positions", dev), _weight(q_weight, D, "q_weight", dev),
+                 _weight(k_weight, D, "k_weight", dev), eps, 2 * pairs, interleaved, 0)
 
 
-def _rows(out: Optional[torch.Tensor], like: torch.Tensor, shape: Tuple[int, ...], name: str) -> torch.Tensor:
+def _rows(out: Optional[torch.Tensor], like: torch.Tensor, shape: Tuple[int, ...], name: str, dev: int) -> torch.Tensor:
     """A contiguous bf16 output, the caller's or a new one on the device of `like` (bf16)."""
     if out is None:
         return like.new_empty(shape) if type(like) is torch.Tensor else torch.empty(shape, dtype=_BF16, device=like.device)
     if out.dtype is not _BF16 or out.shape != shape or not out.is_contiguous():
         raise ValueError(f"{name}: contiguous bf16 {tuple(shape)}")
+    if out.get_device() != dev:
+        raise _elsewhere(name, out, dev)
     return out
+
+
+def _room(ws: Optional[torch.Tensor], dev: int) -> Tuple[Optional[int], int]:
+    """Address and bytes of a workspace."""
+    if ws is None:
+        return None, 0
+    if ws.get_device() != dev:
+        raise _elsewhere("ws", ws, dev)
+    return ws.data_ptr(), ws.numel()
 
 
 def rope_frequencies(rot: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
@@ -531,6 +569,7 @@ def rope_frequencies(rot: int, base: float = 10000.0, scaling: Optional[str] = N
 def rope_table(length: int, inv_freq: torch.Tensor, magnitude: float = 1.0, device="cuda") -> torch.Tensor:
     """cos and sin of m * inv_freq[i] for m < length, angles in fp64: fp32 [length, pairs, 2]."""
     f = inv_freq.to(device=device, dtype=torch.float64).contiguous()
+    _require(f.get_device() >= 0, "a table is made on a GPU")
     table = torch.empty((length, f.numel(), 2), dtype=torch.float32, device=f.device)
     _check(LIB.fq_rope_table(_p(f), magnitude, length, f.numel(), _p(table), _stream()))
     return table
@@ -545,18 +584,20 @@ def qk_rope(q: torch.Tensor, k: Optional[torch.Tensor], table: Optional[torch.Te
     multiples of 8 -> contiguous (q_out, k_out).  positions int32 [T] (None: 0, 1, ...)."""
     shape = q.shape
     T, Hq, D = shape
-    rope = _rope_desc(table, positions, T, q_weight, k_weight, D, eps, interleaved)
-    hq, hk, Hk, yk = _heads(q, "q"), None, 0, None
-    yq = _rows(q_out, q, shape, "q_out")
+    dev = q.get_device()
+    rope = _rope_desc(table, positions, T, q_weight, k_weight, D, eps, interleaved, dev)
+    hq, hk, Hk, yk = _heads(q, "q", dev), None, 0, None
+    yq = _rows(q_out, q, shape, "q_out", dev)
     if k is not None:
         shape = k.shape
         Hk = shape[1]
         if shape != (T, Hk, D):
             raise ValueError("k: [T, Hk, D] of q's T and D")
-        hk, yk = _heads(k, "k"), _rows(k_out, k, shape, "k_out")
-    rc = LIB.fq_qk_rope(hq, Hq, hk, Hk, rope, T, D, yq.data_ptr(), None if yk is None else yk.data_ptr(), _stream_handle())
+        hk, yk = _heads(k, "k", dev), _rows(k_out, k, shape, "k_out", dev)
+    to_q, to_k = (yq, yk) if dev >= 0 else (q, k)  # (_refuse)
+    rc = LIB.fq_qk_rope(hq, Hq, hk, Hk, rope, T, D, to_q.data_ptr(), None if to_k is None else to_k.data_ptr(), _stream_handle())
     if rc:
-        _check(rc)
+        _refuse(rc, dev)
     return yq, yk
 
 
@@ -571,20 +612,23 @@ def cache_append(cache: KVCache, page_table: torch.Tensor, q_start: torch.Tensor
     max_new: the most rows of a sequence.  positions: None for a token's place in its sequence."""
     shape = k.shape
     T, H, D = shape
-    desc, ch, P, cd = _cache_desc(cache)
+    dev = k.get_device()
+    desc, ch, P, cd = _cache_desc(cache, dev)
     if H != ch or D != cd or v.shape != shape:
         raise ValueError("k, v: [T, heads, D] of the cache's heads and D")
-    batch = _batch_desc(page_table, q_start, kv_len, max_new, page_table.shape[1] * P if page_table.dim() == 2 else 0)
+    batch = _batch_desc(page_table, q_start, kv_len, max_new, page_table.shape[1] * P if page_table.dim() == 2 else 0, dev)
     y, Hq, hq = None, 0, None
     if q is not None:
         shape = q.shape
         Hq = shape[1]
         if shape != (T, Hq, D):
             raise ValueError("q: [T, Hq, D] of k's T and D")
-        hq, y = _heads(q, "q"), _rows(q_out, q, shape, "q_out")
-    rope = _rope_desc(table, positions, T, q_weight, k_weight, D, eps, interleaved)
-    rc = LIB.fq_cache_append(desc, batch, _heads(k, "k"), _heads(v, "v"), hq, Hq, rope, T, None if y is None else y.data_ptr(),
-                             _stream_handle())
+        hq, y = _heads(q, "q", dev), _rows(q_out, q, shape, "q_out", dev)
+    rope = _rope_desc(table, positions, T, q_weight, k_weight, D, eps, interleaved, dev)
+    hk, hv = _heads(k, "k", dev), _heads(v, "v", dev)
+    if dev < 0:
+        raise ValueError("the tensors are on the host, not on a GPU")
+    rc = LIB.fq_cache_append(desc, batch, hk, hv, hq, Hq, rope, T, None if y is None else y.data_ptr(), _stream_handle())
     if rc:
         _check(rc)
     return y
@@ -593,8 +637,9 @@ def cache_append(cache: KVCache, page_table: torch.Tensor, q_start: torch.Tensor
 def cache_read(cache: KVCache, page_table: torch.Tensor, first: torch.Tensor, last: torch.Tensor, max_tokens: int,
                k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Tokens first[b] .. last[b] - 1 of every sequence as values: bf16 k, v [seqs, max_tokens, heads, D], zeros beyond."""
-    desc, H, _, D = _cache_desc(cache)
-    B, width = _table_shape(page_table)
+    dev = page_table.get_device()
+    desc, H, _, D = _cache_desc(cache, dev)
+    B, width = _table_shape(page_table, dev)
     shape = (B, max_tokens, H, D)
     if k_out is None or v_out is None:
         new = torch.empty((2, *shape), dtype=_BF16, device=page_table.device)
@@ -602,8 +647,13 @@ def cache_read(cache: KVCache, page_table: torch.Tensor, first: torch.Tensor, la
     for o, name in ((k_out, "k_out"), (v_out, "v_out")):
         if o.dtype is not _BF16 or o.shape != shape or not o.is_contiguous():
             raise ValueError(f"{name}: contiguous bf16 {shape}")
-    rc = LIB.fq_cache_read(desc, page_table.data_ptr(), width, _index(first, B, "first"), _index(last, B, "last"), B, max_tokens,
-                           k_out.data_ptr(), v_out.data_ptr(), _stream_handle())
+        if o.get_device() != dev:
+            raise _elsewhere(name, o, dev)
+    lo, hi = _index(first, B, "first", dev), _index(last, B, "last", dev)
+    if dev < 0:
+        raise ValueError("the tensors are on the host, not on a GPU")
+    rc = LIB.fq_cache_read(desc, page_table.data_ptr(), width, lo, hi, B, max_tokens, k_out.data_ptr(), v_out.data_ptr(),
+                           _stream_handle())
     if rc:
         _check(rc)
     return k_out, v_out
@@ -621,17 +671,20 @@ def cache_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, q
     1/sqrt(D); causal: a row sees the tokens up to its own place, otherwise all kv_len[b]."""
     shape = q.shape
     T, Hq, D = shape
-    desc, H, _, cd = _cache_desc(cache)
+    dev = q.get_device()
+    desc, H, _, cd = _cache_desc(cache, dev)
     if D != cd:
         raise ValueError("q: [T, Hq, D] of the cache's D")
-    batch = _batch_desc(page_table, q_start, kv_len, max_new, max_kv)
-    hq, y = _heads(q, "q"), _rows(out, q, shape, "out")
+    batch = _batch_desc(page_table, q_start, kv_len, max_new, max_kv, dev)
+    hq, y = _heads(q, "q", dev), _rows(out, q, shape, "out", dev)
     if ws is None:
         ws = _scratch(LIB.fq_cache_attention_workspace_bytes(T, Hq, H, D, page_table.shape[0], max_new, max_kv), q.device)
-    rc = LIB.fq_cache_attention(hq, Hq, T, desc, batch, D ** -0.5 if scale is None else scale, causal, y.data_ptr(),
-                                None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream_handle())
+    room, size = _room(ws, dev)
+    to = y if dev >= 0 else q  # (_refuse)
+    rc = LIB.fq_cache_attention(hq, Hq, T, desc, batch, D ** -0.5 if scale is None else scale, causal, to.data_ptr(), room, size,
+                                _stream_handle())
     if rc:
-        _check(rc)
+        _refuse(rc, dev)
     return y
 
 
@@ -647,6 +700,7 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kv_len: O
     unseen places has no effect; a sample that sees nothing gives zeros."""
     shape, ks = q.shape, k.shape
     B, Sq, Hq, D = shape
+    dev = q.get_device()
     _, Sk, Hk, _ = ks
     if ks != (B, Sk, Hk, D) or v.shape != ks:
         raise ValueError("k, v: [B, Sk, Hk, D] of q's B and D")
@@ -655,13 +709,16 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kv_len: O
         if (key_mask.dtype not in (torch.bool, torch.uint8) or key_mask.shape != (B, Sk)
                 or (Sk > 1 and key_mask.stride(1) != 1)):
             raise ValueError("key_mask: bool [B, Sk] with unit stride of the last dim")
+        if key_mask.get_device() != dev:
+            raise _elsewhere("key_mask", key_mask, dev)
         mask, stride = key_mask.data_ptr(), key_mask.stride(0)
-    hq, y = _heads(q, "q"), _rows(out, q, shape, "out")
+    hq, hk, hv, y = _heads(q, "q", dev), _heads(k, "k", dev), _heads(v, "v", dev), _rows(out, q, shape, "out", dev)
     if ws is None:
         ws = _scratch(LIB.fq_cross_attention_workspace_bytes(B, Sq, Sk, Hq, Hk, D), q.device)
-    rc = LIB.fq_cross_attention(hq, _heads(k, "k"), _heads(v, "v"), _index(kv_len, B, "kv_len") or None, mask or None, stride, B, Sq,
-                                Sk, Hq, Hk, D, D ** -0.5 if scale is None else scale, y.data_ptr(),
-                                None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream_handle())
+    room, size = _room(ws, dev)
+    to = y if dev >= 0 else q  # (_refuse)
+    rc = LIB.fq_cross_attention(hq, hk, hv, _index(kv_len, B, "kv_len", dev) or None, mask or None, stride, B, Sq, Sk, Hq, Hk, D,
+                                D ** -0.5 if scale is None else scale, to.data_ptr(), room, size, _stream_handle())
     if rc:
-        _check(rc)
+        _refuse(rc, dev)
     return y
