@@ -221,7 +221,9 @@ __global__ __launch_bounds__(64, DP == 256 ? 1 : 2) void attention_stream_kernel
     }
     // Weights enter the product as two bf16 values each, 16 bits of them: the matrix unit has the time
     // while the keys and values come from memory.  (With one, the result's error against 64 bits is
-    // 0.0024 of its size for 0.0016, bf16's own, and the times are the same within 2 %.)
+    // 0.0024 of its size for 0.0016, bf16's own, and the times are the same within 2 %.)  Values of states may
+    // be infinite: their weights are cut off, not rounded, and the second value is at least 2^-24 of the weight, so
+    // that neither meets an infinity with another sign or as 0 (15 bits).  A cache's codes are finite.
     uint4 p[NB / 2], rest[NB / 2];
 #pragma unroll
     for (int b = 0; b < NB / 2; ++b) {
@@ -232,9 +234,14 @@ __global__ __launch_bounds__(64, DP == 256 ? 1 : 2) void attention_stream_kernel
         float w1 = exp2_fast(__builtin_fmaf(st[2 * b + e / 2][2 * (e % 2) + 1], c, -m));
         l += w0;
         l += w1;
-        if (CACHED) w0 *= v, w1 *= v;
-        w[e] = pack_bf16(w0, w1);
-        r[e] = pack_bf16(w0 - bf16_lo(w[e]), w1 - bf16_hi(w[e]));
+        if constexpr (CACHED) {
+          w0 *= v, w1 *= v;
+          w[e] = pack_bf16(w0, w1);
+          r[e] = pack_bf16(w0 - bf16_lo(w[e]), w1 - bf16_hi(w[e]));
+        } else {
+          w[e] = __builtin_amdgcn_perm(__float_as_uint(w1), __float_as_uint(w0), 0x07060302u);
+          r[e] = pack_bf16(__builtin_fmaf(w0, 0x1p-24f, w0 - bf16_lo(w[e])), __builtin_fmaf(w1, 0x1p-24f, w1 - bf16_hi(w[e])));
+        }
       }
       p[b] = make_uint4(w[0], w[1], w[2], w[3]);
       rest[b] = make_uint4(r[0], r[1], r[2], r[3]);

@@ -1,4 +1,4 @@
-"""Edges of the attention operators on the GPU: rows past a call's bound."""
+"""Edges of the attention operators on the GPU: rows past a call's bound, values that are not finite."""
 import numpy as np
 import pytest
 import torch
@@ -61,3 +61,33 @@ def test_rows_past_the_bound_leave_the_others_where_they_are(n, lens, most, P):
             k, v = (sequence(table, c, s.cpu().numpy(), b, m, h // 2) for c, s in ((k_now, got.k_scale), (v_now, got.v_scale)))
             at = slice(start[b], start[b] + kept[b])
             check_rows(out[at, h], q[at, h], k, v, seen, D ** -0.5, f"sequence {b} head {h}")
+
+
+SIZES = [(1, 100), (1, 1500), (5, 700), (400, 1500)]
+
+
+@pytest.mark.parametrize("D", [64, 80, 128, 256])
+@pytest.mark.parametrize("Sq,Sk", SIZES)
+def test_an_infinite_value_is_an_infinite_mean(Sq, Sk, D):
+    f = fq()
+    flush(f"infinite values Sq={Sq} Sk={Sk} D={D}")
+    rng = np.random.default_rng(Sq + D)
+    Hq, H = 4, 2
+    q, qt = bf16(rng.standard_normal((1, Sq, Hq, D)) * 0.5)
+    k, kt = bf16(rng.standard_normal((1, Sk, H, D)) * 0.5)
+    v = rng.standard_normal((1, Sk, H, D))
+    v[0, 7, 0, 3], v[0, 40, 0, 9], v[0, Sk - 1, 1, 5] = np.inf, -np.inf, -np.inf
+    v, vt = bf16(v)
+    out = f.cross_attention(qt, kt, vt)
+    want = torch.zeros((H, D))
+    want[0, 3], want[0, 9], want[1, 5] = np.inf, -np.inf, -np.inf
+    for h in range(Hq):
+        w = want[h // 2]
+        there = torch.isinf(w)
+        assert (out[0, :, h].float().cpu()[:, there] == w[there]).all()
+        finite = np.where(np.isfinite(v[0, :, h // 2]), v[0, :, h // 2], 0.0)
+        got = out[0, :, h].clone()
+        got[:, there.to(DEV)] = 0
+        other = finite.copy()
+        other[:, there.numpy()] = 0
+        check_rows(got, q[0, :, h], k[0, :, h // 2], other, np.ones((Sq, Sk), dtype=bool), D ** -0.5, f"head {h}")
