@@ -432,6 +432,7 @@ __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_k
   float ks0 = 0.0f, ks1 = 0.0f, vs0 = 0.0f, vs1 = 0.0f;  // scales of this tile's groups and the next's
   auto bits_of = [&](uint32_t mask) { return CACHED ? ~0ull : __ballot(mask != 0); };
   uint64_t bits = ~0ull;  // seen places of the tile after this one
+  uint64_t seen = 0;      // of all tiles
   if (tiles > 0) {
     // keys 0 and 1 and values 0 into LDS, values 1 and keys 2 under way
     if constexpr (CACHED) look_up(0);
@@ -452,6 +453,7 @@ __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_k
     for (int n = 0; n < kKeyPieces; ++n) stage_key(keys_at, n);
     hold = in;
     bits = bits_of(hold.mask);
+    seen = bits0 | bits;
     ks1 = in.ks;
     vs0 = in.vs;
     load(1);
@@ -489,6 +491,7 @@ __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_k
     if constexpr (!CACHED) {
       clear_rows(hold.v, bits);
       bits = bits_of(hold.mask);
+      seen |= bits;
       clear_rows(hold.k, bits);
     }
     half_tile(sa, sb, vb, 0, k0, t, 1, [&](int n) { return key_operand(k1, 0, n); }, ValuePieces{},
@@ -505,6 +508,16 @@ __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_k
     if (t + 1 == tiles) break;
     tile(t + 1, std::integral_constant<int, 1>{});
   }
+  // Where nothing is seen the results are zeros, also for a query that is not finite, whose products with the
+  // zeros of unseen places are not.  (`seen` has tiles behind this part's too: where those hold the only seen
+  // places, another part has them and such a query's row is NaN as it should be.)
+  if (!CACHED && seen == 0)
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+      l[x][0] = l[x][1] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i) o[x][i] = f32x16{};
+    }
 #pragma unroll
   for (int x = 0; x < RT; ++x) {
     const float sum = across32(l[x][0] + l[x][1], [](float y, float z) { return y + z; });

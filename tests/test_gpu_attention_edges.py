@@ -1,4 +1,4 @@
-"""Edges of the attention operators on the GPU: rows past a call's bound, values that are not finite."""
+"""Edges of the attention operators on the GPU: rows past a call's bound, values and queries that are not finite."""
 import numpy as np
 import pytest
 import torch
@@ -91,3 +91,23 @@ def test_an_infinite_value_is_an_infinite_mean(Sq, Sk, D):
         other = finite.copy()
         other[:, there.numpy()] = 0
         check_rows(got, q[0, :, h], k[0, :, h // 2], other, np.ones((Sq, Sk), dtype=bool), D ** -0.5, f"head {h}")
+
+
+@pytest.mark.parametrize("D", [64, 80, 128, 256])
+@pytest.mark.parametrize("Sq,Sk", SIZES)
+def test_a_sample_that_sees_nothing_is_zeros_whatever_its_queries_hold(Sq, Sk, D):
+    f = fq()
+    flush(f"nothing seen Sq={Sq} Sk={Sk} D={D}")
+    rng = np.random.default_rng(Sq + D)
+    B, Hq, H = 3, 4, 2
+    q = rng.standard_normal((B, Sq, Hq, D))
+    q[1, 0] = rng.choice([np.nan, np.inf, -np.inf], (Hq, D))
+    q[1, Sq - 1, 2, 3] = np.nan
+    q[2, Sq // 2, 1, 0] = np.nan
+    kv = bf16(rng.standard_normal((B, Sk, 2 * H, D)))[1]
+    mask = rng.random((B, Sk)) < 0.5
+    mask[1] = False
+    out = f.cross_attention(bf16(q)[1], kv[:, :, :H], kv[:, :, H:], None, torch.from_numpy(mask).to(DEV))
+    assert (out[1] == 0).all()
+    nan = torch.isnan(out).cpu().numpy()
+    assert nan[2, Sq // 2, 1].all() and nan.any(axis=3).sum() == 1
