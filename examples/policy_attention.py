@@ -3,7 +3,8 @@
   1. the language layers read 816 prefix tokens: W4A4 q|k|v projection, head norms, rotation and an append to an 8-bit
      cache in one call, causal attention over the cache, W8A8 output projection;
   2. the action expert denoises 50 action tokens: its layers append them behind the prefix (the same slots at every
-     step) and attend to everything in the cache, every token seeing every other;
+     step, the first of them in a copy of the prefix's last page) and attend to everything in the cache, every token
+     seeing every other;
   3. a second expert reads the language states by cross attention (keys and values projected once for all steps).
 
     python examples/policy_attention.py [--layers 2] [--steps 4] [--prefix 816] [--actions 50]
@@ -59,37 +60,64 @@ class CrossLayer:
         return x + self.o(a.view(x.shape[0], self.heads * self.head_dim))
 
 
+class Policy:
+    """A prompt read once into the caches, then denoising steps over it.
+
+    An append to a page that is in use may raise the page's scale, which rounds the earlier tokens' codes again, and a page
+    given a value that is not finite is lost as a whole.  The steps write the same slots over and over, the first of them
+    behind the prompt's last tokens: their page is a copy, made anew at every step, and the prompt's own stays as it was read."""
+
+    def __init__(self, layers, prefix, actions, page, gen):
+        total = prefix + actions
+        per_seq = -(-total // page)
+        self.prefix, self.actions = prefix, actions
+        # the language model's heads and the expert's share a cache: 8 query heads on one key head of 256
+        self.language = [CachedLayer(2048, 8, 1, 256, gen) for _ in range(layers)]
+        self.expert = [CachedLayer(1024, 8, 1, 256, gen) for _ in range(layers)]
+        self.cross = CrossLayer(1024, 2048, 16, 64, gen)
+        self.caches = [fq.kv_cache(per_seq + 1, 1, page, 256) for _ in range(layers)]
+        inv_freq, magnitude = fq.rope_frequencies(256)
+        self.rope = fq.rope_table(total, inv_freq, magnitude)
+        order = torch.randperm(per_seq + 1, generator=gen, device="cuda").to(torch.int32)
+        self.pages, self.step_pages = order[None, :per_seq].contiguous(), order[None, :per_seq].clone()
+        self.shared = None  # (the prompt's last page, the steps' copy of it)
+        if prefix % page:
+            self.shared = int(order[prefix // page]), int(order[per_seq])
+            self.step_pages[0, prefix // page] = order[per_seq]
+        ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+        self.prompt_batch = (self.pages, ints(0, prefix), ints(prefix))
+        self.step_batch = (self.step_pages, ints(0, actions), ints(total))
+
+    def read(self, x, mask=None):
+        """The prompt's tokens through the language layers; mask: the places that the second expert sees."""
+        for layer, cache in zip(self.language, self.caches):
+            x = layer(x, cache, self.prompt_batch, self.rope, self.prefix, self.prefix, True)
+        self.states, self.mask = self.cross.states(x), mask
+        return x
+
+    def velocity(self, y):
+        """One step's direction for the actions y."""
+        z = y
+        for layer, cache in zip(self.expert, self.caches):
+            if self.shared is not None:
+                kept, copy = self.shared
+                for t in cache:
+                    t[copy] = t[kept]
+            z = layer(z, cache, self.step_batch, self.rope, self.actions, self.prefix + self.actions, False)
+        return self.cross(z, self.states, self.mask)
+
+
 def run(layers=2, steps=4, prefix=816, actions=50, page=64, seed=0):
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
-    total = prefix + actions
-    per_seq = -(-total // page)
-    # the language model's heads and the expert's share a cache: 8 query heads on one key head of 256
-    language = [CachedLayer(2048, 8, 1, 256, gen) for _ in range(layers)]
-    expert = [CachedLayer(1024, 8, 1, 256, gen) for _ in range(layers)]
-    cross = CrossLayer(1024, 2048, 16, 64, gen)
-    caches = [fq.kv_cache(per_seq, 1, page, 256) for _ in range(layers)]
-    inv_freq, magnitude = fq.rope_frequencies(256)
-    rope = fq.rope_table(total, inv_freq, magnitude)
-    pages = torch.randperm(per_seq, generator=gen, device="cuda").to(torch.int32)[None]
-    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
-
+    policy = Policy(layers, prefix, actions, page, gen)
     x = torch.randn((prefix, 2048), generator=gen, device="cuda").to(torch.bfloat16)
-    batch = (pages, ints(0, prefix), ints(prefix))
-    for layer, cache in zip(language, caches):
-        x = layer(x, cache, batch, rope, prefix, prefix, True)
-    states = cross.states(x)
-    mask = torch.rand((1, prefix), generator=gen, device="cuda") < 0.9  # places of absent camera images are unseen
-
+    # places of absent camera images are unseen
+    x = policy.read(x, torch.rand((1, prefix), generator=gen, device="cuda") < 0.9)
     y = torch.randn((actions, 1024), generator=gen, device="cuda").to(torch.bfloat16)
-    batch = (pages, ints(0, actions), ints(total))
     for _ in range(steps):
-        z = y
-        for layer, cache in zip(expert, caches):
-            z = layer(z, cache, batch, rope, actions, total, False)
-        z = cross(z, states, mask)
-        y = y - z / steps
-    return y, x, caches, pages
+        y = y - policy.velocity(y) / steps
+    return y, x, policy.caches, policy.pages
 
 
 def main():

@@ -356,6 +356,8 @@ fq_status fq_qk_rope(const fq_heads *q, int Hq, const fq_heads *k, int Hk, const
  * A scale below the smallest normal fp32 is 0, its codes too.  A page given a value that is
  * not finite gets the scale NaN: what attends to any of its tokens (of that head) is NaN.
  * Slots of the page beyond the last token hold unspecified codes.
+ * Writing slots again, behind tokens that stay, is an append like any other: the page keeps a scale that the
+ * overwritten tokens raised, and NaN.  Tokens that will be written again want pages of their own, or a copy of the page.
  * q (or NULL, with Hq = 0 and q_out = NULL): normed and rotated into q_out [T, Hq, D] in the
  * same launch.  rope may be NULL: no norm and no rotation.  T >= q_start[seqs]. */
 fq_status fq_cache_append(const fq_kv_cache *cache, const fq_kv_batch *batch, const fq_heads *k, const fq_heads *v,
