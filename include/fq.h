@@ -309,14 +309,16 @@ typedef struct {
  *   k_codes  int8 [pages, heads, P, D]         k_scale  fp32 [pages, heads]
  *   v_codes  int8 [pages, heads, P/16, D, 16]  v_scale  fp32 [pages, heads]
  * (the tokens of a group of 16 are adjacent in v_codes: the order in which the product with
- * the attention weights sums them).  A value is code * scale. */
+ * the attention weights sums them).  A value is code * scale.
+ *   growth   0 to 100: where an append has to raise a scale over earlier tokens, it raises it by this many
+ *            percent at least (see fq_cache_append; nothing else reads it) */
 typedef struct {
   void *k_codes;
   float *k_scale;
   void *v_codes;
   float *v_scale;
   int64_t pages;
-  int32_t heads, page_tokens, head_dim, reserved;
+  int32_t heads, page_tokens, head_dim, growth;
 } fq_kv_cache;
 
 /* A ragged batch of sequences over a cache, all int32 device arrays (4-byte aligned, as
@@ -350,12 +352,21 @@ fq_status fq_qk_rope(const fq_heads *q, int Hq, const fq_heads *k, int Hk, const
  * slot kv_len[b] - n_b + i (n_b = q_start[b+1] - q_start[b]; a row whose slot is negative is dropped), its
  * keys normed and rotated, its values as they are.  For every
  * page and head that new tokens reach, with a = max |x| over them in fp32:
- *   scale' = a / 127, or max(scale, a / 127) where the page holds earlier tokens;
+ *   scale' = a / 127; where the page holds earlier tokens: scale if a / 127 <= scale, or else
+ *            max(a / 127, scale * (1 + growth / 100));
  *   earlier codes = rne(code * (scale / scale')) where the scale grew;
  *   new codes = clamp(rne(x * (1 / scale')), -127, 127).
  * A scale below the smallest normal fp32 is 0, its codes too.  A page given a value that is
  * not finite gets the scale NaN: what attends to any of its tokens (of that head) is NaN.
  * Slots of the page beyond the last token hold unspecified codes.
+ * A token is within half a step (scale) of its value when it is written, and every later raise of its page's
+ * scale adds up to half a step of that raise's.  A page written by one call is within half a step; one filled
+ * token by token within half the sum of the scales it went through: up to P / 2 of its last steps if every
+ * token raises it a little (codes that a small raise rounds to themselves drift with the scale), 1 to 2 for
+ * normal values.  With growth > 0 the raises are a geometric series and the bound is
+ * (1 + growth/100) / (growth/50) of the last scale whatever P is (2.5 at 25, 1.5 at 50, 1 at 100), that scale at most
+ * 1 + growth/100 of what the page's values need.  Appending a page's tokens again from its first slot rounds
+ * them once.
  * Writing slots again, behind tokens that stay, is an append like any other: the page keeps a scale that the
  * overwritten tokens raised, and NaN.  Tokens that will be written again want pages of their own, or a copy of the page.
  * q (or NULL, with Hq = 0 and q_out = NULL): normed and rotated into q_out [T, Hq, D] in the

@@ -21,9 +21,10 @@ def norm_rotate(x, table=None, positions=None, weight=None, eps=1e-6, interleave
     return y
 
 
-def append_page(new, codes, scale, held):
+def append_page(new, codes, scale, held, growth=0):
     """One page of one head: `new` fp32 [n, D] goes behind `held` earlier tokens of codes int8 [P, D] under
-    fp32 `scale`.  Returns (codes, scale) after the append, in fp32 arithmetic; slots beyond are as they were."""
+    fp32 `scale`, which grows by `growth` percent at least where it has to.  Returns (codes, scale) after the append, in
+    fp32 arithmetic; slots beyond are as they were."""
     f = np.float32
     codes = codes.copy()
     if len(new) == 0:
@@ -34,7 +35,7 @@ def append_page(new, codes, scale, held):
         return codes, f(np.nan)
     s = f(a / f(127))
     if held:
-        s = max(f(scale), s)
+        s = f(scale) if f(scale) >= s else max(s, f(f(scale) * f(f(1) + f(growth) / f(100))))
     if s < np.finfo(f).tiny:
         s = f(0)
     if held and s != f(scale) and s > 0:

@@ -29,6 +29,7 @@ struct Cache {
   float *vs;
   int64_t pages;
   int H, P, D;
+  float growth;  // of a scale that has to grow, at least
 };
 
 struct Batch {

@@ -107,7 +107,7 @@ fq_status check_cache(const fq_kv_cache *c, Cache *out) {
   if (!aligned16(c->k_codes) || !aligned16(c->k_scale) || !aligned16(c->v_codes) || !aligned16(c->v_scale))
     return fail(FQ_ERR_ALIGN, "pointers must be 16-byte aligned");
   *out = Cache{static_cast<int8_t *>(c->k_codes), c->k_scale, static_cast<int8_t *>(c->v_codes), c->v_scale, c->pages,
-               c->heads, P, c->head_dim};
+               c->heads, P, c->head_dim, 1.0f};
   return FQ_OK;
 }
 
@@ -218,6 +218,8 @@ fq_status fq_cache_append(const fq_kv_cache *cache, const fq_kv_batch *batch, co
   Rope r;
   Heads hk, hv, hq{};
   if ((s = check_cache(cache, &c)) != FQ_OK) return s;
+  if (cache->growth < 0 || cache->growth > 100) return fail(FQ_ERR_UNSUPPORTED, "growth=%d outside [0, 100]", cache->growth);
+  c.growth = 1.0f + (float)cache->growth / 100.0f;
   if ((s = check_batch(batch, c, &b)) != FQ_OK) return s;
   if ((s = check_count("T", T, kMaxTokens)) != FQ_OK) return s;
   if ((s = check_count("Hq", Hq, kMaxHeads)) != FQ_OK) return s;

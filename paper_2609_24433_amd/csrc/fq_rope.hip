@@ -231,7 +231,9 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t *lds) {
 
 // Workgroups [0, kv_items): one page of one sequence and head, keys or values.  The page's new tokens
 // are read once, NP a lane group, and stay in registers as they came: their largest value gives the
-// scale, then they become codes.  The others: the query heads of the new tokens.
+// scale, then they become codes.  A scale that has to grow grows by c.growth at least: each growth rounds the
+// earlier codes once more, and codes that a ratio near 1 leaves as they are drift with the scale.  The other
+// workgroups: the query heads of the new tokens.
 template <int L, int NP>
 __global__ __launch_bounds__(kThreads) void cache_append_kernel(Cache c, Batch b, Heads k, Heads v, Heads q, int Hq,
                                                                 int Sq, int64_t kv_items, int pages_per_seq,
@@ -306,7 +308,7 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(Cache c, Batch b
   bool bad = top >= 0x7F800000u;
   if (held) {
     bad = bad || old != old;
-    scale = old > scale ? old : scale;
+    scale = old >= scale ? old : __builtin_fmaxf(scale, old * c.growth);
   }
   if (!(scale >= FLT_MIN)) scale = 0.0f;
   const bool grew = held && !bad && scale != old;

@@ -479,7 +479,7 @@ def _weight(w: Optional[torch.Tensor], D: int, name: str, dev: int) -> int:
     return w.data_ptr()
 
 
-def _cache_desc(c: KVCache, dev: int) -> Tuple[bytes, int, int, int]:
+def _cache_desc(c: KVCache, dev: int, growth: int = 0) -> Tuple[bytes, int, int, int]:
     kc, ks, vc, vs = c
     pages, H, P, D = kc.shape
     if (kc.dtype is not _I8 or vc.dtype is not _I8 or vc.shape != (pages, H, P // 16, D, 16) or not kc.is_contiguous()
@@ -491,7 +491,7 @@ def _cache_desc(c: KVCache, dev: int) -> Tuple[bytes, int, int, int]:
     for t in c:
         if t.get_device() != dev:
             raise _elsewhere("the cache", t, dev)
-    return _CACHE(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), pages, H, P, D, 0), H, P, D
+    return _CACHE(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), pages, H, P, D, growth), H, P, D
 
 
 def _table_shape(page_table: torch.Tensor, dev: int) -> Tuple[int, int]:
@@ -605,15 +605,18 @@ def cache_append(cache: KVCache, page_table: torch.Tensor, q_start: torch.Tensor
                  k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
                  table: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
                  q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
-                 interleaved: bool = False, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+                 interleaved: bool = False, q_out: Optional[torch.Tensor] = None, growth: int = 0) -> Optional[torch.Tensor]:
     """Appends the tokens of a ragged batch (rows q_start[b] .. q_start[b+1] - 1 of k, v [T, Hk, D] are the last ones of
     the kv_len[b] tokens of sequence b) to its pages: keys normed and rotated as by qk_rope, keys and values rounded to 8
     bits under a scale per page and head.  q [T, Hq, D] is normed and rotated in the same launch and returned.
-    max_new: the most rows of a sequence.  positions: None for a token's place in its sequence."""
+    max_new: the most rows of a sequence.  positions: None for a token's place in its sequence.
+    growth: percent that a page's scale grows at least, where it has to grow over earlier tokens.  Every growth rounds
+    the earlier tokens again: a page filled token by token errs by up to half a step for each with 0 (2 steps for
+    normal values, tens for values that keep rising a little), by 2.5 steps at most with 25."""
     shape = k.shape
     T, H, D = shape
     dev = k.get_device()
-    desc, ch, P, cd = _cache_desc(cache, dev)
+    desc, ch, P, cd = _cache_desc(cache, dev, growth)
     if H != ch or D != cd or v.shape != shape:
         raise ValueError("k, v: [T, heads, D] of the cache's heads and D")
     batch = _batch_desc(page_table, q_start, kv_len, max_new, page_table.shape[1] * P if page_table.dim() == 2 else 0, dev)
