@@ -34,8 +34,10 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // tokens a part, 19 with 128, 28 with 256.
 // Tiles: 256 rows a workgroup of eight waves where there are more than 128 rows and the head size
 // leaves the registers (head 128, 4096 rows over 8190 tokens: 414 us, with 128 rows 444), one a
-// compute unit; two of 128 rows fit otherwise.  Tokens are split only to fill the card, 128 or more
-// a part.
+// compute unit; of 128 rows two fit with heads of up to 128, one above (139 KB of LDS).  Tokens are
+// split only to fill the card once, 128 or more a part: 8 query heads on one key head of 256, 816 tokens over 1632
+// take 39 us, split for two workgroups a unit 50, 4096 over 4096 158 and 181; 1500 over 6000, head 160,
+// 135 and 122, where 94 row tiles leave a quarter of the card idle.
 Plan plan_attention(bool cached, int Hq, int Hk, int D, int64_t seqs, int64_t max_new, int64_t max_kv) {
   Plan p;
   const int64_t rows = max_new * (Hq / Hk);
@@ -50,7 +52,7 @@ Plan plan_attention(bool cached, int Hq, int Hk, int D, int64_t seqs, int64_t ma
     if (chunk < least) chunk = least;
     while (chunk > 64 && groups * ceil_div(max_kv, chunk) < 1024) chunk = ceil_div(chunk / 2, 64) * 64;
   } else {
-    const int64_t want = p.rows == 256 ? 256 : 512, splits = groups >= want ? 1 : want / groups;
+    const int64_t want = p.rows == 256 || D > 128 ? 256 : 512, splits = groups >= want ? 1 : want / groups;
     chunk = ceil_div(ceil_div(max_kv, splits), 128) * 128;
   }
   p.splits = max_kv > chunk ? (int)ceil_div(max_kv, chunk) : 1;
