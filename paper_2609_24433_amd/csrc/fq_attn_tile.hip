@@ -38,11 +38,11 @@ __device__ __forceinline__ int swizzle(int token) {
   return DP == 64 ? ((token >> 1) & 3) | ((token >> 2) & 4) : (token & 7) | ((token >> 1) & 8);
 }
 
-template <bool CACHED, int DP, int RT, int WAVES>
+template <bool CACHED, int DP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_kernel(AttnArgs a, Split sp, int row_tiles) {
   extern __shared__ __align__(16) uint8_t lds[];
   using L = Lds<CACHED, DP>;
-  constexpr int kThreads = 64 * WAVES, kRows = 32 * RT * WAVES;
+  constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
   constexpr int KU = kTile * (DP / 16) / kThreads;  // 16-channel pieces of keys a thread stages
   constexpr int VU = CACHED ? 4 * DP / kThreads : kTile * (DP / 8) / kThreads;
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -64,37 +64,28 @@ __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_k
   if (c1 <= c0 && part > 0) return;  // no row of it has a partial result here
   const int tiles = c1 > c0 ? (c1 - c0 + kTile - 1) / kTile : 0;
 
-  // this lane's rows, one of each block, as the column of both products
-  bool live[RT];
-  int qi[RT], hq[RT], end[RT], end_min[RT];  // end_min: least that a row of the block sees
-  bf16x8 q[RT][DP / 16];
-#pragma unroll
-  for (int x = 0; x < RT; ++x) {
-    const int b0 = r0 + (wave * RT + x) * 32, r = b0 + col;
-    live[x] = r < total;
-    qi[x] = live[x] ? r / G : 0;
-    hq[x] = h * G + (live[x] ? r - qi[x] * G : 0);
-    end[x] = live[x] ? rows.end(qi[x]) : 0;
-    end_min[x] = b0 < total ? rows.end(b0 / G) : 0;
-    const uint16_t *p = CACHED ? a.q.p + (rows.q0 + qi[x]) * a.q.ts + hq[x] * a.q.hs
-                               : a.q.p + s * a.q.bs + qi[x] * a.q.ts + hq[x] * a.q.hs;
+  // this lane's row, as the column of both products
+  const int b0 = r0 + wave * 32, row = b0 + col;
+  const bool live = row < total;
+  const int qi = live ? row / G : 0;
+  const int hq = h * G + (live ? row - qi * G : 0);
+  const int end = live ? rows.end(qi) : 0;
+  const int least = b0 < total ? rows.end(b0 / G) : 0;  // that any row of the wave sees
+  bf16x8 q[DP / 16];
+  {
+    const uint16_t *p = CACHED ? a.q.p + (rows.q0 + qi) * a.q.ts + hq * a.q.hs : a.q.p + s * a.q.bs + qi * a.q.ts + hq * a.q.hs;
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) {
       uint4 u = make_uint4(0, 0, 0, 0);
-      if (live[x] && 16 * i < D) u = *reinterpret_cast<const uint4 *>(p + 16 * i + 8 * half);
-      q[x][i] = __builtin_bit_cast(bf16x8, u);
+      if (live && 16 * i < D) u = *reinterpret_cast<const uint4 *>(p + 16 * i + 8 * half);
+      q[i] = __builtin_bit_cast(bf16x8, u);
     }
   }
 
-  f32x16 o[RT][DP / 32];
-  float m[RT], l[RT][2];  // l: of even and odd tokens
+  f32x16 o[DP / 32];
 #pragma unroll
-  for (int x = 0; x < RT; ++x) {
-#pragma unroll
-    for (int i = 0; i < DP / 32; ++i) o[x][i] = f32x16{};
-    m[x] = -FLT_MAX;
-    l[x][0] = l[x][1] = 0.0f;
-  }
+  for (int i = 0; i < DP / 32; ++i) o[i] = f32x16{};
+  float m = -FLT_MAX, l[2] = {0.0f, 0.0f};  // l: of even and odd tokens
   const float c_all = a.scale * 1.4426950408889634f;
 
   // Loads of the tiles to come.  Every load is unconditional, at an address that is there (channels
@@ -261,8 +252,7 @@ __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_k
       return make_uint4(v0.x, v0.y, v1.x, v1.y);
     }
   };
-  // STEPS operands, each used for every block of rows, with `work` (step, block) behind each matrix
-  // instruction; the reads run on into the operands of the next chain.  The walls hold the order:
+  // STEPS operands and products, with `work` (step) behind each matrix instruction; the reads run on into the operands of the next chain.  The walls hold the order:
   // left alone the compiler reads all operands at once, for which there are no registers, or gathers
   // the vector work behind the products.
   uint4 ring[AHEAD + 1];
@@ -276,12 +266,9 @@ __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_k
     auto step = [&](auto at) {
       constexpr int n = decltype(at)::value;
       ring[(n + AHEAD) % (AHEAD + 1)] = n + AHEAD < STEPS ? operand(n + AHEAD) : next_operand(n + AHEAD - STEPS);
-      auto block = [&](auto bx) {
-        product(n, decltype(bx)::value, __builtin_bit_cast(bf16x8, ring[n % (AHEAD + 1)]));
-        work(std::integral_constant<int, n * RT + decltype(bx)::value>{});
-        sched_wall();
-      };
-      static_for<RT>(block);
+      product(n, __builtin_bit_cast(bf16x8, ring[n % (AHEAD + 1)]));
+      work(at);
+      sched_wall();
     };
     static_for<STEPS>(step);
   };
@@ -299,109 +286,90 @@ __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_k
   // -infinity, with the scale applied here, so that a scale that is 0 or NaN reaches only what is
   // seen; a NaN scale of the values goes by the scores.
   struct Scores {
-    f32x16 st[RT];
-    float c[RT], v[RT], top[RT];
+    f32x16 st;
+    float c, v, top;
   };
   auto begin = [&](Scores &z, int t, int b, float ks, float vs) {
+    if constexpr (CACHED) {
+      z.st = f32x16{};
+    } else {
+      const float4 *p = reinterpret_cast<const float4 *>(bias + (t & 3) * kTile + 32 * b + 16 * half);
 #pragma unroll
-    for (int x = 0; x < RT; ++x) {
-      if constexpr (CACHED) {
-        z.st[x] = f32x16{};
-      } else {
-        const float4 *p = reinterpret_cast<const float4 *>(bias + (t & 3) * kTile + 32 * b + 16 * half);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float4 f = p[e];
-          z.st[x][4 * e] = f.x, z.st[x][4 * e + 1] = f.y, z.st[x][4 * e + 2] = f.z, z.st[x][4 * e + 3] = f.w;
-        }
+      for (int e = 0; e < 4; ++e) {
+        const float4 f = p[e];
+        z.st[4 * e] = f.x, z.st[4 * e + 1] = f.y, z.st[4 * e + 2] = f.z, z.st[4 * e + 3] = f.w;
       }
-      z.c[x] = CACHED ? c_all * ks : c_all;
-      z.v[x] = CACHED ? vs : 1.0f;
     }
+    z.c = CACHED ? c_all * ks : c_all;
+    z.v = CACHED ? vs : 1.0f;
   };
-  int least = end_min[0];  // that any row of the wave sees
-#pragma unroll
-  for (int x = 1; x < RT; ++x) least = end_min[x] < least ? end_min[x] : least;
   auto hide_unseen = [&](Scores &z, int t, int b) {
     const int j0 = c0 + t * kTile + 32 * b;
-    if (CACHED && j0 + 32 > least)
+    if (CACHED && j0 + 32 > least) {
+      const int left = end - (j0 + 16 * half);
+      const uint32_t on = left >= 16 ? 0xFFFFu : left <= 0 ? 0u : (1u << left) - 1;
+      const float bad = z.v - z.v;
 #pragma unroll
-      for (int x = 0; x < RT; ++x) {
-        const int left = end[x] - (j0 + 16 * half);
-        const uint32_t on = left >= 16 ? 0xFFFFu : left <= 0 ? 0u : (1u << left) - 1;
-        const float bad = z.v[x] - z.v[x];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) z.st[x][e] = (on >> e & 1) ? __builtin_fmaf(z.st[x][e], z.c[x], bad) : -INFINITY;
-        z.c[x] = 1.0f;
-        z.v[x] = bad == 0.0f ? z.v[x] : 1.0f;
-      }
+      for (int e = 0; e < 16; ++e) z.st[e] = (on >> e & 1) ? __builtin_fmaf(z.st[e], z.c, bad) : -INFINITY;
+      z.c = 1.0f;
+      z.v = bad == 0.0f ? z.v : 1.0f;
+    }
   };
-  // maximum of a lane's scores, two at a time: piece n of 8 RT
+  // maximum of a lane's scores, two at a time: piece n of 8
   auto two_maxima = [&](Scores &z, int n) {
-    const int x = n % RT, y = n / RT;
-    const float t0 = maxf(z.st[x][2 * y], z.st[x][2 * y + 1]);
-    z.top[x] = y == 0 ? t0 : maxf(z.top[x], t0);
-    asm volatile("" : "+v"(z.top[x]));
+    const float t0 = maxf(z.st[2 * n], z.st[2 * n + 1]);
+    z.top = n == 0 ? t0 : maxf(z.top, t0);
+    asm volatile("" : "+v"(z.top));
   };
   // The running maximum moves only where it has to: a weight up to 2^8 is as exact as one up to 1.
   auto follow_maximum = [&](const Scores &z) {
-    bool above = false;
-    float top[RT];
+    const float top = z.top * z.c;
+    if (__any(top > m + 8.0f)) {
+      const float to = maxf(m, across32(maxf(top, -FLT_MAX), maxf)), shrink = exp2_fast(m - to);
+      m = to;
+      l[0] *= shrink;
+      l[1] *= shrink;
 #pragma unroll
-    for (int x = 0; x < RT; ++x) {
-      top[x] = z.top[x] * z.c[x];
-      above = above || top[x] > m[x] + 8.0f;
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] *= shrink;
     }
-    if (__any(above))
-#pragma unroll
-      for (int x = 0; x < RT; ++x) {
-        const float to = maxf(m[x], across32(maxf(top[x], -FLT_MAX), maxf)), shrink = exp2_fast(m[x] - to);
-        m[x] = to;
-        l[x][0] *= shrink;
-        l[x][1] *= shrink;
-#pragma unroll
-        for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[x][i][e] *= shrink;
-      }
   };
-  uint4 w[RT][2];  // weights in the operand order of the second product
-  // Two scores to weights: piece n of 8 RT + 1, all blocks' first 8 tokens before their last 8.  The
-  // exponentials of a piece come with the sums and conversions of the one before, whose results
-  // they would otherwise wait for.
+  uint4 w[2];  // weights in the operand order of the second product
+  // Two scores to weights: piece n of 8 + 1.  The exponentials of a piece come with the sums and
+  // conversions of the one before, whose results they would otherwise wait for.
   float e0 = 0.0f, e1 = 0.0f;
   auto two_weights = [&](const Scores &z, int n) {
     const float p0 = e0, p1 = e1;
-    if (n < 8 * RT) {
-      const int x = n / 4 % RT, y = n / (4 * RT) * 4 + n % 4;
-      e0 = exp2_fast(__builtin_fmaf(z.st[x][2 * y], z.c[x], -m[x]));
-      e1 = exp2_fast(__builtin_fmaf(z.st[x][2 * y + 1], z.c[x], -m[x]));
+    if (n < 8) {
+      e0 = exp2_fast(__builtin_fmaf(z.st[2 * n], z.c, -m));
+      e1 = exp2_fast(__builtin_fmaf(z.st[2 * n + 1], z.c, -m));
     }
     if (n > 0) {
-      const int k = n - 1, x = k / 4 % RT, y = k / (4 * RT) * 4 + k % 4;
+      const int y = n - 1;
       // Weights enter the product as bf16, with the scale of the values in them: 9 bits of each, as the
       // result will have.  What the rounding drops would take a second product, and matrix instructions
       // bound the kernel.
       uint32_t u;
       if constexpr (CACHED) {
-        l[x][0] += p0;
-        l[x][1] += p1;
-        u = pack_bf16(p0 * z.v[x], p1 * z.v[x]);
+        l[0] += p0;
+        l[1] += p1;
+        u = pack_bf16(p0 * z.v, p1 * z.v);
       } else {  // the sum of the weights as they are used
         u = pack_bf16(p0, p1);
-        l[x][n % 2] = add_pair(u, l[x][n % 2]);
+        l[n % 2] = add_pair(u, l[n % 2]);
       }
-      asm volatile("" : "+v"(u), "+v"(l[x][0]), "+v"(l[x][1]));  // here, not where the weights are used
-      uint4 &to = w[x][y / 4];
+      asm volatile("" : "+v"(u), "+v"(l[0]), "+v"(l[1]));  // here, not where the weights are used
+      uint4 &to = w[y / 4];
       (y % 4 == 0 ? to.x : y % 4 == 1 ? to.y : y % 4 == 2 ? to.z : to.w) = u;
     }
     asm volatile("" : "+v"(e0), "+v"(e1));
   };
-  auto output_product = [&](int n, int x, bf16x8 u) {
+  auto output_product = [&](int n, bf16x8 u) {
     const int i = n % (DP / 32);
-    o[x][i] = mfma32(u, __builtin_bit_cast(bf16x8, w[x][n / (DP / 32)]), o[x][i]);
+    o[i] = mfma32(u, __builtin_bit_cast(bf16x8, w[n / (DP / 32)]), o[i]);
   };
-  constexpr int kWeights = 8 * RT + 1, kMaxima = 8 * RT, kLength = STEPS * RT;
+  constexpr int kWeights = 9, kMaxima = 8;
   // weights left for the first half of the second chain, whose products need only the first half
   constexpr int kLate = kWeights * 5 / 16;
 
@@ -411,13 +379,13 @@ __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_k
                        auto following, auto pieces, auto stage) {
     auto values = [&](int n) { return value_operand(vb, b, n); };
     chain([&](int n) { return key_operand(kb, b_next, n); }, values,
-          [&](int n, int x, bf16x8 k) { next.st[x] = mfma32(k, q[x][n], next.st[x]); },
-          [&](auto at) { share(at, 0, kLength, kWeights - kLate, [&](int n) { two_weights(now, n); }); });
+          [&](int n, bf16x8 k) { next.st = mfma32(k, q[n], next.st); },
+          [&](auto at) { share(at, 0, STEPS, kWeights - kLate, [&](int n) { two_weights(now, n); }); });
     hide_unseen(next, t_next, b_next);
     chain(values, following, output_product, [&](auto at) {
-      share(at, 0, kLength / 2, kLate, [&](int n) { two_weights(now, kWeights - kLate + n); });
-      share(at, kLength / 8, kLength, kMaxima, [&](int n) { two_maxima(next, n); });
-      share(at, kLength / 2, kLength, decltype(pieces)::value, stage);
+      share(at, 0, STEPS / 2, kLate, [&](int n) { two_weights(now, kWeights - kLate + n); });
+      share(at, STEPS / 8, STEPS, kMaxima, [&](int n) { two_maxima(next, n); });
+      share(at, STEPS / 2, STEPS, decltype(pieces)::value, stage);
     });
     follow_maximum(next);
   };
@@ -471,7 +439,7 @@ __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_k
     auto first = [&](int n) { return key_operand(keys_at, 0, n); };
     prime(first);
     chain(first, [&](int n) { return key_operand(keys_at, 1, n); },
-          [&](int n, int x, bf16x8 k) { sa.st[x] = mfma32(k, q[x][n], sa.st[x]); }, [](auto) {});
+          [&](int n, bf16x8 k) { sa.st = mfma32(k, q[n], sa.st); }, [](auto) {});
     hide_unseen(sa, 0, 0);
 #pragma unroll
     for (int n = 0; n < kMaxima; ++n) two_maxima(sa, n);
@@ -511,64 +479,58 @@ __global__ __launch_bounds__(64 * WAVES, DP < 256 ? 2 : 1) void attention_tile_k
   // Where nothing is seen the results are zeros, also for a query that is not finite, whose products with the
   // zeros of unseen places are not.  (`seen` has tiles behind this part's too: where those hold the only seen
   // places, another part has them and such a query's row is NaN as it should be.)
-  if (!CACHED && seen == 0)
+  if (!CACHED && seen == 0) {
+    l[0] = l[1] = 0.0f;
 #pragma unroll
-    for (int x = 0; x < RT; ++x) {
-      l[x][0] = l[x][1] = 0.0f;
-#pragma unroll
-      for (int i = 0; i < DP / 32; ++i) o[x][i] = f32x16{};
-    }
-#pragma unroll
-  for (int x = 0; x < RT; ++x) {
-    const float sum = across32(l[x][0] + l[x][1], [](float y, float z) { return y + z; });
-    if (!live[x]) continue;
-    // a lane holds channels 32 i + 8 y + 4 half + z of its row
-    if (sp.splits > 1) {
-      const int64_t at = (((int64_t)part * a.seqs + s) * a.Hk + h) * (a.max_new * G) + r0 + (wave * RT + x) * 32 + col;
-      if (half == 0) sp.ml[at] = make_float2(m[x], sum);
-#pragma unroll
-      for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const int d = 32 * i + 8 * y + 4 * half;
-          if (d < D)
-            *reinterpret_cast<float4 *>(sp.o + at * D + d) =
-                make_float4(o[x][i][4 * y], o[x][i][4 * y + 1], o[x][i][4 * y + 2], o[x][i][4 * y + 3]);
-        }
-      continue;
-    }
-    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-    uint16_t *out = a.out + ((rows.q0 + qi[x]) * a.Hq + hq[x]) * D;
+    for (int i = 0; i < DP / 32; ++i) o[i] = f32x16{};
+  }
+  const float sum = across32(l[0] + l[1], [](float y, float z) { return y + z; });
+  if (!live) return;
+  // a lane holds channels 32 i + 8 y + 4 half + z of its row
+  if (sp.splits > 1) {
+    const int64_t at = (((int64_t)part * a.seqs + s) * a.Hk + h) * (a.max_new * G) + row;
+    if (half == 0) sp.ml[at] = make_float2(m, sum);
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
         const int d = 32 * i + 8 * y + 4 * half;
         if (d < D)
-          *reinterpret_cast<uint2 *>(out + d) = make_uint2(pack_bf16(o[x][i][4 * y] * inv, o[x][i][4 * y + 1] * inv),
-                                                          pack_bf16(o[x][i][4 * y + 2] * inv, o[x][i][4 * y + 3] * inv));
+          *reinterpret_cast<float4 *>(sp.o + at * D + d) = make_float4(o[i][4 * y], o[i][4 * y + 1], o[i][4 * y + 2], o[i][4 * y + 3]);
       }
+    return;
   }
+  const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+  uint16_t *out = a.out + ((rows.q0 + qi) * a.Hq + hq) * D;
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const int d = 32 * i + 8 * y + 4 * half;
+      if (d < D)
+        *reinterpret_cast<uint2 *>(out + d) = make_uint2(pack_bf16(o[i][4 * y] * inv, o[i][4 * y + 1] * inv),
+                                                        pack_bf16(o[i][4 * y + 2] * inv, o[i][4 * y + 3] * inv));
+    }
 }
 
-template <bool CACHED, int DP, int RT, int WAVES>
+template <bool CACHED, int DP, int WAVES>
 hipError_t launch(const AttnArgs &a, const Split &sp, hipStream_t s) {
   static std::atomic<uint64_t> raised{0};
   const size_t lds = Lds<CACHED, DP>::kBytes;
-  hipError_t e = allow_dynamic_lds(attention_tile_kernel<CACHED, DP, RT, WAVES>, lds, raised);
+  hipError_t e = allow_dynamic_lds(attention_tile_kernel<CACHED, DP, WAVES>, lds, raised);
   if (e != hipSuccess) return e;
-  const int rows = 32 * RT * WAVES;
+  const int rows = 32 * WAVES;
   const int64_t row_tiles = (a.max_new * (a.Hq / a.Hk) + rows - 1) / rows;
-  attention_tile_kernel<CACHED, DP, RT, WAVES>
+  attention_tile_kernel<CACHED, DP, WAVES>
       <<<dim3((unsigned)(a.Hk * row_tiles * sp.splits), (unsigned)a.seqs), 64 * WAVES, lds, s>>>(a, sp, (int)row_tiles);
   return hipGetLastError();
 }
 
 template <bool CACHED>
 hipError_t launch_size(const AttnArgs &a, const Split &sp, int rows, hipStream_t s) {
-  if (a.D <= 64) return launch<CACHED, 64, 1, 4>(a, sp, s);
-  if (a.D <= 128) return rows > 128 ? launch<CACHED, 128, 1, 8>(a, sp, s) : launch<CACHED, 128, 1, 4>(a, sp, s);
-  return launch<CACHED, 256, 1, 4>(a, sp, s);
+  if (a.D <= 64) return launch<CACHED, 64, 4>(a, sp, s);
+  if (a.D <= 128) return rows > 128 ? launch<CACHED, 128, 8>(a, sp, s) : launch<CACHED, 128, 4>(a, sp, s);
+  return launch<CACHED, 256, 4>(a, sp, s);
 }
 
 }  // namespace
