@@ -135,7 +135,7 @@ __global__ void rope_table_kernel(const double *__restrict__ f, double magnitude
   table[i] = make_float2((float)(magnitude * c), (float)(magnitude * s));
 }
 
-// One token's heads slice, slice + S, ... of H: its angles and weights stay in registers.
+// One token's heads slice, slice + S, ... of H (S = H: one): its angles and weights stay in registers.
 template <int L>
 __device__ __forceinline__ void rope_heads(const uint16_t *x, int64_t hs, uint16_t *y, int H, int slice, int S,
                                            const Rope &r, const float *w, const Place &p, const float2 (&cs)[8], int D) {
@@ -149,23 +149,22 @@ __device__ __forceinline__ void rope_heads(const uint16_t *x, int64_t hs, uint16
   }
 }
 
-// Grid: units of (token, slice); a token has Sq slices of query heads, then Sk of key heads.
+// Grid: units of (token, head), query heads before key heads.
 template <int L>
-__global__ __launch_bounds__(kThreads) void qk_rope_kernel(Heads q, int Hq, int Sq, Heads k, int Hk, int Sk, Rope r,
-                                                           int64_t T, int D, uint16_t *__restrict__ q_out,
-                                                           uint16_t *__restrict__ k_out) {
+__global__ __launch_bounds__(kThreads) void qk_rope_kernel(Heads q, int Hq, Heads k, int Hk, Rope r, int64_t T, int D,
+                                                           uint16_t *__restrict__ q_out, uint16_t *__restrict__ k_out) {
   const int64_t u = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
-  const int S = Sq + Sk, m = threadIdx.x % L;
-  const int64_t t = u / S;
+  const int H = Hq + Hk, m = threadIdx.x % L;
+  const int64_t t = u / H;
   if (t >= T) return;
-  const int slice = (int)(u - t * S);
+  const int h = (int)(u - t * H);
   const Place p = place_of(m, D, r.rot, r.interleaved);
   float2 cs[8];
   load_angles(r, p, m, r.positions ? r.positions[t] : t, cs);
-  if (slice < Sq)
-    rope_heads<L>(q.p + t * q.ts, q.hs, q_out + t * Hq * D, Hq, slice, Sq, r, r.qw, p, cs, D);
+  if (h < Hq)
+    rope_heads<L>(q.p + t * q.ts, q.hs, q_out + t * Hq * D, Hq, h, Hq, r, r.qw, p, cs, D);
   else
-    rope_heads<L>(k.p + t * k.ts, k.hs, k_out + t * Hk * D, Hk, slice - Sq, Sk, r, r.kw, p, cs, D);
+    rope_heads<L>(k.p + t * k.ts, k.hs, k_out + t * Hk * D, Hk, h - Hq, Hk, r, r.kw, p, cs, D);
 }
 
 // ---------------------------------------------------------------- appends
@@ -476,10 +475,10 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(Cache c, const int
 
 // Heads of a token that one lane group takes in turn, with the token's angles and the weights in
 // registers: up to `most`, where there are groups enough to fill the card (eight waves a SIMD).
-int slices(int64_t tokens, int heads_all, int H, int L, int most) {
+int slices(int64_t tokens, int H, int L, int most) {
   if (H == 0) return 0;
   int per = most;
-  while (per > 1 && tokens * ((heads_all + per - 1) / per) * L / 64 < 8192) per /= 2;
+  while (per > 1 && tokens * ((H + per - 1) / per) * L / 64 < 8192) per /= 2;
   return (H + per - 1) / per;
 }
 
@@ -513,9 +512,8 @@ hipError_t launch_qk_rope(const Heads &q, int Hq, const Heads &k, int Hk, const 
                           uint16_t *q_out, uint16_t *k_out, hipStream_t s) {
   return with_lanes(D, [&](auto l) {
     constexpr int L = decltype(l)::value;
-    const int Sq = Hq, Sk = Hk;
-    const int64_t blocks = (T * (Sq + Sk) + kThreads / L - 1) / (kThreads / L);
-    qk_rope_kernel<L><<<dim3((unsigned)blocks), kThreads, 0, s>>>(q, Hq, Sq, k, Hk, Sk, r, T, D, q_out, k_out);
+    const int64_t blocks = (T * (Hq + Hk) + kThreads / L - 1) / (kThreads / L);
+    qk_rope_kernel<L><<<dim3((unsigned)blocks), kThreads, 0, s>>>(q, Hq, k, Hk, r, T, D, q_out, k_out);
     return hipGetLastError();
   });
 }
@@ -526,7 +524,7 @@ hipError_t launch_cache_append(const Cache &c, const Batch &b, const Heads &k, c
     constexpr int L = decltype(l)::value;
     const int pages = (int)((b.max_new + 2 * c.P - 2) / c.P);  // pages that max_new tokens can reach
     const int64_t kv_items = b.seqs * pages * c.H * 2;
-    const int Sq = slices(b.seqs * b.max_new, Hq, Hq, L, 8);
+    const int Sq = slices(b.seqs * b.max_new, Hq, L, 8);
     const int64_t q_blocks = Hq ? (b.max_new * Sq + kThreads / L - 1) / (kThreads / L) : 0;
     const unsigned blocks = (unsigned)(kv_items + b.seqs * q_blocks);
     const size_t lds = (size_t)c.P * c.D / 16 * 17;
