@@ -276,7 +276,10 @@ fq_status fq_gptq_sweep(const float *w_t, int64_t ldw, const double *U, int64_t 
  *   fq_cross_attention  attention to bf16 keys and values of another length
  * Shapes: query heads Hq, key heads Hk with Hq a multiple of Hk (query head h reads key head
  * h / (Hq / Hk)), both at most 1024; head size D a multiple of 16 in [16, 256]; the rotary part R a multiple of 16,
- * 0 <= R <= D.  Queries, keys and values are bf16; statistics, softmax and sums are fp32. */
+ * 0 <= R <= D.  Queries, keys and values are bf16; statistics, softmax and sums are fp32.  The attention
+ * weights enter their product with the values with 15 bits or more where a call has few query rows a key head
+ * (by its bounds max_new and max_kv, or Sq and Sk), and with 8 where it has many: the same row may differ by
+ * 2^-8 of its weighted mean of |v| between two such calls, as a bf16 result does by its own rounding. */
 
 /* bf16 rows of heads: element d of head h of token t (of sequence b) at
  * p[b batch_stride + t token_stride + h head_stride + d], strides in elements, multiples of
@@ -370,7 +373,7 @@ fq_status fq_qk_rope(const fq_heads *q, int Hq, const fq_heads *k, int Hk, const
  * Writing slots again, behind tokens that stay, is an append like any other: the page keeps a scale that the
  * overwritten tokens raised, and NaN.  Tokens that will be written again want pages of their own, or a copy of the page.
  * q (or NULL, with Hq = 0 and q_out = NULL): normed and rotated into q_out [T, Hq, D] in the
- * same launch.  rope may be NULL: no norm and no rotation.  T >= q_start[seqs]. */
+ * same launch (rows that no sequence has, and those past max_new, are not written).  rope may be NULL: no norm and no rotation.  T >= q_start[seqs]. */
 fq_status fq_cache_append(const fq_kv_cache *cache, const fq_kv_batch *batch, const fq_heads *k, const fq_heads *v,
                           const fq_heads *q, int Hq, const fq_head_rope *rope, int64_t T, void *q_out, void *stream);
 
@@ -383,7 +386,8 @@ fq_status fq_cache_read(const fq_kv_cache *cache, const int32_t *page_table, int
 
 /* out bf16 [T, Hq, D] = softmax(scale q k^T) v per row over the cache: row i of a sequence
  * of n rows sees tokens j < kv_len, and j <= kv_len - n + i where `causal`.  A row that sees
- * nothing gives zeros.  scale > 0.  ws: fq_cache_attention_workspace_bytes bytes (partial
+ * nothing gives zeros; rows of out that no sequence has, and those past max_new, are not written.
+ * scale > 0.  ws: fq_cache_attention_workspace_bytes bytes (partial
  * results where a sequence's tokens are split over workgroups; 0 and NULL where they are
  * not), no initialization. */
 size_t fq_cache_attention_workspace_bytes(int64_t T, int Hq, int Hk, int D, int64_t seqs, int64_t max_new,
