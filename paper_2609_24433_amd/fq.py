@@ -488,9 +488,8 @@ def _cache_desc(c: KVCache, dev: int, growth: int = 0) -> Tuple[bytes, int, int,
     if (ks.dtype is not _F32 or vs.dtype is not _F32 or ks.shape != (pages, H) or vs.shape != (pages, H)
             or not ks.is_contiguous() or not vs.is_contiguous()):
         raise ValueError("cache scales: contiguous fp32 [pages, heads]")
-    for t in c:
-        if t.get_device() != dev:
-            raise _elsewhere("the cache", t, dev)
+    if kc.get_device() != dev or ks.get_device() != dev or vc.get_device() != dev or vs.get_device() != dev:
+        raise _elsewhere("the cache", next(t for t in c if t.get_device() != dev), dev)
     return _CACHE(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), pages, H, P, D, growth), H, P, D
 
 
@@ -644,14 +643,11 @@ def cache_read(cache: KVCache, page_table: torch.Tensor, first: torch.Tensor, la
     desc, H, _, D = _cache_desc(cache, dev)
     B, width = _table_shape(page_table, dev)
     shape = (B, max_tokens, H, D)
-    if k_out is None or v_out is None:
-        new = torch.empty((2, *shape), dtype=_BF16, device=page_table.device)
-        k_out, v_out = new[0] if k_out is None else k_out, new[1] if v_out is None else v_out
-    for o, name in ((k_out, "k_out"), (v_out, "v_out")):
-        if o.dtype is not _BF16 or o.shape != shape or not o.is_contiguous():
-            raise ValueError(f"{name}: contiguous bf16 {shape}")
-        if o.get_device() != dev:
-            raise _elsewhere(name, o, dev)
+    if k_out is None and v_out is None:
+        k_out, v_out = torch.empty((2, *shape), dtype=_BF16, device=page_table.device)
+    else:
+        given = v_out if k_out is None else k_out
+        k_out, v_out = _rows(k_out, given, shape, "k_out", dev), _rows(v_out, given, shape, "v_out", dev)
     lo, hi = _index(first, B, "first", dev), _index(last, B, "last", dev)
     if dev < 0:
         raise ValueError("the tensors are on the host, not on a GPU")
