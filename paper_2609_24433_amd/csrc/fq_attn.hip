@@ -33,7 +33,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // where there are too few to fill the card: one sequence of 877 tokens, head 256, takes 10 us with 64
 // tokens a part, 19 with 128, 28 with 256.
 // Tiles: 256 rows a workgroup of eight waves where there are more than 128 rows and the head size
-// leaves the registers (head 128, 4096 rows over 8190 tokens: 414 us, with 128 rows 444), one a
+// leaves the registers (head 128, 4096 rows over 8190 tokens: 422 us, with 128 rows 457), one a
 // compute unit; of 128 rows two fit with heads of up to 128, one above (139 KB of LDS).  Tokens are
 // split only to fill the card once, 128 or more a part: 8 query heads on one key head of 256, 816 tokens over 1632
 // take 39 us, split for two workgroups a unit 50, 4096 over 4096 158 and 181; 1500 over 6000, head 160,
@@ -63,8 +63,8 @@ Plan plan_attention(bool cached, int Hq, int Hk, int D, int64_t seqs, int64_t ma
 // A row's result from its parts, 4 channels a lane: `lanes` lanes a part, `ways` parts of a row at
 // once (each way keeps its own maximum).  A workgroup has 256 / (lanes ways)
 // units; a unit is a row, or with fewer lanes than channels / 4 a slice of its channels.  Bound by the
-// latency of its loads: 32 rows of 512 parts, head 128, 8.4 MB, 6.3 us (the ways joined one after another
-// through LDS: 10.7); 8 rows of 14 parts, 4 us, mostly launch.
+// latency of its loads: 32 rows of 512 parts, head 128, 8.4 MB, 6.3 us, 0.2 of its waves' time vector work (the ways
+// joined one after another through LDS: 10.7 us); 8 rows of 14 parts, 3.5 to 4.6 us, mostly launch.
 template <bool CACHED>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, Split sp, int log_lanes, int log_ways, int slices) {
   __shared__ float4 os[256];

@@ -10,10 +10,12 @@
 //                            values (first half: of the next tile) or keys (second: the one after)
 // Loads run a tile ahead of the staging.
 //
-// Measured, with the join: 4096 tokens over 8190 in the cache, causal, 32 query heads on 8 of 128: 411
-// us, 1.00 PFLOP/s, 0.8 of what a plain product of 8192^3 reaches (the pipeline alone, its operands
-// left in LDS, 358 us); 4 samples of 1031 queries over up to 4099 masked bf16 states, 16 heads on 8 of
-// 128: 149 us (94 alone: the longest sample's workgroups run with part of the card idle).
+// Measured, with the join: 4096 tokens over 8190 in the cache, causal, 32 query heads on 8 of 128: 400 to
+// 434 us by the card, 1.0 PFLOP/s, 0.8 of what a plain product of 8192^3 reaches, the matrix units busy for
+// 0.45 of the time under counters (on a card where it takes 422 us, 361 without loads and staging); 4 samples of 1031 queries over up to 4099 masked
+// bf16 states, 16 heads on 8 of 128: 148 us, as long as its two long samples (4099 and 3514 states) take
+// alone: their 144 workgroups run with the rest of the card idle.  Heads above 128 run one wave a SIMD: 4096
+// causal tokens, 8 query heads on one of 256, 150 us, 0.46 PFLOP/s, and 816 tokens 30 us.
 #include "fq_attn_device.hpp"
 #include "fq_attn_launch.hpp"
 

@@ -7,11 +7,12 @@
 // fp32 from the bf16 input to the one rounding at the end.
 //
 // All are bound by memory where they are long and by launches and the latency of dependent loads
-// where they are short.  Measured: norm and rotation of 16385 tokens, 40 heads of 128: 78 us, 4.4 TB/s; of
-// 50 tokens, 9 heads of 256: 4.1 us.  Append of a prompt of 16383 tokens, 32 query and 8 key heads of
-// 128: 94 us, 4.4 TB/s; of one token to each of 32 sequences: 6 us, of which most is a page's chain of
-// waits (lengths, table entry, scale, codes).  Read of the last page of each
-// of 32 sequences: 8 us; of 16383 tokens, 8 heads of 128: 23 us, 4.3 TB/s.
+// where they are short.  Measured: norm and rotation of 16385 tokens, 40 heads of 128: 74 to 79 us by the
+// card (71 in a kernel trace), 4.3 to 4.6 TB/s; of 50 tokens, 9 heads of 256: 4.1 us.  Append of a prompt of 16383
+// tokens, 32 query and 8 key heads of 128: 95 us, 4.3 TB/s; of one token to each of 32 sequences: 6.5 us where no
+// page's scale grows, 8.4 where every page's does, most of it a page's chain of waits (lengths, table entry,
+// scale, codes).  Read of the last page of each of 32 sequences: 8 us; of 16383 tokens, 8 heads of 128: 23 us, 4.3
+// TB/s.
 #include <cfloat>
 
 #include "fq_attn.hpp"
