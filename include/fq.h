@@ -406,6 +406,79 @@ fq_status fq_cross_attention(const fq_heads *q, const fq_heads *k, const fq_head
                              const uint8_t *key_mask, int64_t mask_stride, int64_t B, int64_t Sq, int64_t Sk, int Hq,
                              int Hk, int D, float scale, void *out, void *ws, size_t ws_bytes, void *stream);
 
+/* ---- Microscaled 4-bit codes, and the norm before a projection ------------------------------
+ *   fq_norm_quant, fq_norm_mx_quant  residual's addition, root-mean-square norm, rotation, codes
+ *   fq_mx_quant                      tokens or weights to microscaled codes
+ *   fq_read_codes, fq_mx_read        codes as values
+ *   fq_mx_pack, fq_mx_unpack         weights' codes in the product's order and back
+ *   fq_mx_gemm, fq_mx_linear         the product; the projection from bf16 to bf16
+ *
+ * Microscaled codes of rows u of K channels: every 32 adjacent channels are a block with one scale.
+ *   codes   uint8 [M, K/2], channel 2i in the low half of byte i: E2M1, sign (8) and one of the
+ *           magnitudes 0 .5 1 1.5 2 3 4 6 (0 .. 7)
+ *   scales  uint8 [K/128, M, 4]: byte (s, t, j) belongs to channels 128 s + 32 j .. + 31 of row t
+ *           and stands for 2^(byte - 127); 255 is NaN.  (Rows' bytes [M, K/32] in order of channels are the
+ *           same array with its first two dimensions exchanged.)
+ * Rounding of a block, A = max |u|: byte = max(floor(log2 A) - 2, -127) + 127, code = u / 2^(byte - 127)
+ * rounded to the nearest magnitude, ties to the even code, at most 6 (so values within a quarter of a block's
+ * largest may saturate).  A block of zeros has byte 0 and codes 0; one with a value that is not finite has byte
+ * 255 and codes 0, and every product that it enters is NaN.  The sign of a zero code is not specified.
+ * K, N, b and alignment as everywhere; M and N at most 2^24; a row stride is not looked at for one row. */
+
+/* u = post . (c_b H_b (pre . x)): the prologue's butterfly (fp32, its order of stages), c_b the float
+ * nearest 1/sqrt(b), each product one fp32 rounding; then the rounding above.
+ *   x  bf16 [M, ldx] (x_is_f32 = 0, ldx a multiple of 8) or fp32 (a multiple of 4); pre_mult, post_mult
+ *      fp32 [K] or NULL.  Tokens take S^-1 and P^-1; row j of W S R^T P takes w_j, S and P. */
+fq_status fq_mx_quant(const void *x, int x_is_f32, int64_t ldx, const float *pre_mult, const float *post_mult, int64_t M,
+                      int64_t K, int b, void *codes, void *scales, void *stream);
+
+/* values bf16 [M, ldv] = code 2^(byte - 127), exactly; NaN where the byte is 255. */
+fq_status fq_mx_read(const void *codes, const void *scales, int64_t M, int64_t K, void *values_bf16, int64_t ldv, void *stream);
+
+/* The product's order of weight codes: uint8 [N/16, K/128, 4, 16, 16], byte (n, s, j, i, c) is byte
+ * 64 s + 16 j + c of row 16 n + i of the codes.  The scales stay as they are. */
+size_t fq_mx_packed_bytes(int64_t N, int64_t K);
+fq_status fq_mx_pack(const void *codes, int64_t N, int64_t K, void *packed, void *stream);
+fq_status fq_mx_unpack(const void *packed, int64_t N, int64_t K, void *codes, void *stream);
+
+/* y bf16 [M, ldy] = bf16_rne(sum over blocks of 2^(ea + ew - 254) sum a w, plus bias[n]): fp32 sums on the
+ * matrix cores, in an order that the shape fixes (the same call gives the same bits), so within
+ * 2^-23 (K/32 + 8) sum |a w| of the exact sum.  bias: fp32 [N] or NULL.
+ *   ws  scratch of fq_mx_gemm_workspace_bytes bytes (fp32 partial sums of a split K; 0 and NULL allowed
+ *       where K is not split), no initialization.  Calls that share one race unless they are ordered. */
+size_t fq_mx_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
+fq_status fq_mx_gemm(const void *a_codes, const void *a_scales, const void *w_packed, const void *w_scales, const float *bias,
+                     void *y_bf16, int64_t ldy, int64_t M, int64_t N, int64_t K, void *ws, size_t ws_bytes, void *stream);
+
+/* fq_mx_quant of bf16 tokens, then fq_mx_gemm, the same output bit for bit; codes, scales and partial
+ * sums live in ws (fq_mx_linear_workspace_bytes bytes). */
+size_t fq_mx_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+fq_status fq_mx_linear(const void *x_bf16, int64_t ldx, const float *smooth_inv, const float *post_inv, int64_t M, int64_t K,
+                       int64_t N, int b, const void *w_packed, const void *w_scales, const float *bias, void *y_bf16, int64_t ldy,
+                       void *ws, size_t ws_bytes, void *stream);
+
+/* What stands before a projection site: h = bf16_rne(x + residual) (h = x without one); s = the float of
+ * 1 / sqrt(sum h^2 / K + eps), sum and root in fp64; y = (h s) weight, two fp32 roundings; then y through
+ * the prologue's transform and rounding (fq_fwht_quant's contract from the butterfly on: codes int8
+ * [M, K] or nibbles [M, K/2], delta fp32 [M]) or through fq_mx_quant's (codes and scales as above).
+ *   x, residual  bf16 [M, ldx], [M, ldr]; residual may be NULL
+ *   weight       fp32 [K], the norm's gain (times S^-1 where the site folds one); eps > 0
+ *   post_inv     fp32 [K] or NULL, after the rotation
+ *   sum_out      bf16 [M, ld_sum] gets h, or NULL; needs a residual.  It may be x or the residual itself
+ *                (the same address and stride); no other overlap.
+ * A row that holds a value that is not finite, before or after the rotation, has codes 0 and delta NaN (blocks of
+ * byte 255 where its microscaled values are not finite); a row whose q / (r A) overflows has codes 0 and delta 0. */
+fq_status fq_norm_quant(const void *x_bf16, int64_t ldx, const void *residual_bf16, int64_t ldr, const float *weight, float eps,
+                        const float *post_inv, int64_t M, int64_t K, int b, int bits, float clip_ratio, void *sum_out,
+                        int64_t ld_sum, void *codes, float *delta, void *stream);
+fq_status fq_norm_mx_quant(const void *x_bf16, int64_t ldx, const void *residual_bf16, int64_t ldr, const float *weight, float eps,
+                           const float *post_inv, int64_t M, int64_t K, int b, void *sum_out, int64_t ld_sum, void *codes,
+                           void *scales, void *stream);
+
+/* values bf16 [M, ldv] = bf16_rne(code * delta[t]) of fq_fwht_quant's or fq_norm_quant's codes (bits 4 or 8). */
+fq_status fq_read_codes(const void *codes, const float *delta, int64_t M, int64_t K, int bits, void *values_bf16, int64_t ldv,
+                        void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,6 +31,8 @@ EXPORTED = ["fq_fwht_quant", "fq_quantize_weights", "fq_packed_weight_bytes", "f
             "fq_rope_table", "fq_qk_rope", "fq_cache_append", "fq_cache_read",
             "fq_cache_attention_workspace_bytes", "fq_cache_attention",
             "fq_cross_attention_workspace_bytes", "fq_cross_attention",
+            "fq_norm_quant", "fq_norm_mx_quant", "fq_read_codes", "fq_mx_quant", "fq_mx_read", "fq_mx_packed_bytes", "fq_mx_pack",
+            "fq_mx_unpack", "fq_mx_gemm_workspace_bytes", "fq_mx_gemm", "fq_mx_linear_workspace_bytes", "fq_mx_linear",
             "fq_status_string", "fq_last_error"]
 
 
@@ -70,6 +72,15 @@ def _load() -> ctypes.CDLL:
         "fq_cache_read": [desc, vp, i64, vp, vp, i64, i64, vp, vp, vp],
         "fq_cache_attention": [desc, i32, i64, desc, desc, f32, i32, vp, vp, sz, vp],
         "fq_cross_attention": [desc, desc, desc, vp, vp, i64, i64, i64, i64, i32, i32, i32, f32, vp, vp, sz, vp],
+        "fq_norm_quant": [vp, i64, vp, i64, vp, f32, vp, i64, i64, i32, i32, f32, vp, i64, vp, vp, vp],
+        "fq_norm_mx_quant": [vp, i64, vp, i64, vp, f32, vp, i64, i64, i32, vp, i64, vp, vp, vp],
+        "fq_read_codes": [vp, vp, i64, i64, i32, vp, i64, vp],
+        "fq_mx_quant": [vp, i32, i64, vp, vp, i64, i64, i32, vp, vp, vp],
+        "fq_mx_read": [vp, vp, i64, i64, vp, i64, vp],
+        "fq_mx_pack": [vp, i64, i64, vp, vp],
+        "fq_mx_unpack": [vp, i64, i64, vp, vp],
+        "fq_mx_gemm": [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, vp, sz, vp],
+        "fq_mx_linear": [vp, i64, vp, vp, i64, i64, i64, i32, vp, vp, vp, vp, i64, vp, sz, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -84,7 +95,9 @@ def _load() -> ctypes.CDLL:
                        "fq_gptq_sweep_workspace_bytes": [i64, i64],
                        "fq_linear_static_max_workspace_bytes": [],
                        "fq_cache_attention_workspace_bytes": [i64, i32, i32, i32, i64, i64, i64],
-                       "fq_cross_attention_workspace_bytes": [i64, i64, i64, i32, i32, i32]}.items():
+                       "fq_cross_attention_workspace_bytes": [i64, i64, i64, i32, i32, i32],
+                       "fq_mx_packed_bytes": [i64, i64], "fq_mx_gemm_workspace_bytes": [i64, i64, i64],
+                       "fq_mx_linear_workspace_bytes": [i64, i64, i64]}.items():
         fn = getattr(lib, name)
         fn.argtypes = args
         fn.restype = sz
@@ -721,3 +734,259 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kv_len: O
     if rc:
         _refuse(rc, dev)
     return y
+
+
+# ---------------------------------------------------------------- microscaled 4-bit codes, and the norm before a projection
+
+_U8 = torch.uint8
+
+
+def _plain(t: torch.Tensor, dtype, shape, name: str, dev: int) -> int:
+    """Address of a contiguous tensor of this type and shape."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {str(dtype)[6:]} {list(shape)}")
+    if t.get_device() != dev:
+        raise _elsewhere(name, t, dev)
+    return t.data_ptr()
+
+
+def _new(like: torch.Tensor, shape, dtype) -> torch.Tensor:
+    return like.new_empty(shape, dtype=dtype) if type(like) is torch.Tensor else torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _matrix(t: torch.Tensor, dtype, shape, name: str, dev: int) -> Tuple[int, int]:
+    """Address and row stride of rows with unit column stride."""
+    if t.dtype is not dtype or t.shape != shape or (t.numel() and t.stride(1) != 1):
+        raise ValueError(f"{name}: {str(dtype)[6:]} {list(shape)} with unit column stride")
+    if t.get_device() != dev:
+        raise _elsewhere(name, t, dev)
+    return t.data_ptr(), t.stride(0)
+
+
+def _on_gpu(dev: int) -> None:
+    """The call goes to the current device's current stream, whose kernels see that device's tensors."""
+    if dev < 0:
+        raise ValueError("the tensors are on the host, not on a GPU")
+    if dev != torch._C._cuda_getDevice():
+        raise ValueError(f"the tensors are on GPU {dev}, the current device is GPU {torch._C._cuda_getDevice()}")
+
+
+def _values_out(out: Optional[torch.Tensor], codes: torch.Tensor, M: int, K: int, dev: int):
+    if out is None:
+        out = _new(codes, (M, K), _BF16)
+        return out, out.data_ptr(), K
+    return (out, *_matrix(out, _BF16, (M, K), "out", dev))
+
+
+def _norm_args(x, weight, residual, sum_out, post_inv):
+    shape = x.shape
+    M, K = shape
+    dev = x.get_device()
+    at, ld = _matrix(x, _BF16, shape, "x", dev)
+    r = ldr = total = lds = 0
+    stream = x
+    if residual is not None:
+        r, ldr = _matrix(residual, _BF16, shape, "residual", dev)
+        stream = _new(x, shape, _BF16) if sum_out is None else sum_out
+        total, lds = (stream.data_ptr(), K) if sum_out is None else _matrix(sum_out, _BF16, shape, "sum_out", dev)
+    elif sum_out is not None:
+        raise ValueError("sum_out needs a residual")
+    return M, K, dev, at, ld, r or None, ldr, _weight(weight, K, "weight", dev) or None, _weight(post_inv, K, "post_inv", dev) or None, \
+        total or None, lds, stream
+
+
+def norm_quant(x: torch.Tensor, weight: torch.Tensor, b: int, bits: int, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+               clip_ratio: float = 1.0, post_inv: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None,
+               out_codes: Optional[torch.Tensor] = None,
+               out_delta: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """The residual's addition, the root-mean-square norm with its gain `weight` fp32 [K] and the prologue's rotation and
+    rounding, bf16 x, residual [M, K] -> (codes uint8 [M, K*bits/8], delta fp32 [M], the sum bf16 [M, K]; x where there is no
+    residual).  sum_out may be x or the residual itself.  The codes are gemm's."""
+    M, K, dev, at, ld, r, ldr, w, post, total, lds, stream = _norm_args(x, weight, residual, sum_out, post_inv)
+    if out_codes is None:
+        out_codes = _new(x, (M, code_bytes(K, bits)), _U8)
+    codes = _plain(out_codes, _U8, (M, code_bytes(K, bits)), "out_codes", dev)
+    if out_delta is None:
+        out_delta = _new(x, (M,), _F32)
+    delta = _plain(out_delta, _F32, (M,), "out_delta", dev)
+    _on_gpu(dev)
+    rc = LIB.fq_norm_quant(at, ld, r, ldr, w, eps, post, M, K, b, bits, clip_ratio, total, lds, codes, delta, _stream_handle())
+    if rc:
+        _check(rc)
+    return out_codes, out_delta, stream
+
+
+def norm_mx_quant(x: torch.Tensor, weight: torch.Tensor, b: int = 1, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  post_inv: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None,
+                  out_codes: Optional[torch.Tensor] = None,
+                  out_scales: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """norm_quant with microscaled codes: (codes uint8 [M, K/2], scales uint8 [K/128, M, 4], the sum).  The codes are
+    mx_gemm's."""
+    M, K, dev, at, ld, r, ldr, w, post, total, lds, stream = _norm_args(x, weight, residual, sum_out, post_inv)
+    out_codes, codes, out_scales, scales = _mx_out(x, M, K, out_codes, out_scales, dev)
+    _on_gpu(dev)
+    rc = LIB.fq_norm_mx_quant(at, ld, r, ldr, w, eps, post, M, K, b, total, lds, codes, scales, _stream_handle())
+    if rc:
+        _check(rc)
+    return out_codes, out_scales, stream
+
+
+def read_codes(codes: torch.Tensor, delta: torch.Tensor, bits: int, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Codes of fwht_quant or norm_quant, uint8 [M, K*bits/8] with delta fp32 [M], as values bf16 [M, K]."""
+    if bits not in (4, 8):
+        raise ValueError("bits: 4 or 8")
+    M, width = codes.shape
+    K, dev = width * 8 // bits, codes.get_device()
+    out, at, ld = _values_out(out, codes, M, K, dev)
+    c, d = _plain(codes, codes.dtype if codes.dtype is _I8 else _U8, (M, width), "codes", dev), _plain(delta, _F32, (M,), "delta", dev)
+    _on_gpu(dev)
+    rc = LIB.fq_read_codes(c, d, M, K, bits, at, ld, _stream_handle())
+    if rc:
+        _check(rc)
+    return out
+
+
+def _mx_out(x, M, K, codes, scales, dev):
+    cs, ss = (M, K // 2), (K // 128, M, 4)
+    if codes is None:
+        codes = _new(x, cs, _U8)
+    if scales is None:
+        scales = _new(x, ss, _U8)
+    return codes, _plain(codes, _U8, cs, "out_codes", dev), scales, _plain(scales, _U8, ss, "out_scales", dev)
+
+
+def mx_quant(x: torch.Tensor, b: int = 1, pre_mult: Optional[torch.Tensor] = None, post_mult: Optional[torch.Tensor] = None,
+             out_codes: Optional[torch.Tensor] = None,
+             out_scales: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Rows bf16 (tokens) or fp32 (weights) [M, K] through the folds and the block Hadamard, rounded to microscaled codes:
+    (codes uint8 [M, K/2], scales uint8 [K/128, M, 4]).  Tokens: pre_mult = S^-1, post_mult = P^-1; weights: S and P."""
+    M, K = x.shape
+    dev, f32 = x.get_device(), x.dtype is _F32
+    at, ld = _matrix(x, _F32 if f32 else _BF16, (M, K), "x", dev)
+    pre, post = _weight(pre_mult, K, "pre_mult", dev) or None, _weight(post_mult, K, "post_mult", dev) or None
+    out_codes, codes, out_scales, scales = _mx_out(x, M, K, out_codes, out_scales, dev)
+    _on_gpu(dev)
+    rc = LIB.fq_mx_quant(at, f32, ld, pre, post, M, K, b, codes, scales, _stream_handle())
+    if rc:
+        _check(rc)
+    return out_codes, out_scales
+
+
+def _mx_codes(codes, scales, name, dev) -> Tuple[int, int, int, int]:
+    """(M, K, address of the codes, of the scales) of microscaled rows."""
+    M, half = codes.shape
+    K = 2 * half
+    return M, K, _plain(codes, _U8, (M, half), name, dev), _plain(scales, _U8, (K // 128, M, 4), name + "'s scales", dev)
+
+
+def mx_read(codes: torch.Tensor, scales: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Microscaled codes as values: bf16 [M, K], exactly."""
+    dev = codes.get_device()
+    M, K, c, s = _mx_codes(codes, scales, "codes", dev)
+    out, at, ld = _values_out(out, codes, M, K, dev)
+    _on_gpu(dev)
+    rc = LIB.fq_mx_read(c, s, M, K, at, ld, _stream_handle())
+    if rc:
+        _check(rc)
+    return out
+
+
+def mx_pack(codes: torch.Tensor) -> torch.Tensor:
+    """Weight codes uint8 [N, K/2] in the product's order: uint8 [N/16, K/128, 4, 16, 16].  The scales stay as they are."""
+    N, half = codes.shape
+    dev = codes.get_device()
+    c = _plain(codes, _U8, (N, half), "codes", dev)
+    out = _new(codes, (N // 16, half // 64, 4, 16, 16), _U8)
+    _on_gpu(dev)
+    _check(LIB.fq_mx_pack(c, N, 2 * half, out.data_ptr(), _stream_handle()))
+    return out
+
+
+def mx_unpack(packed: torch.Tensor) -> torch.Tensor:
+    """mx_pack's inverse."""
+    n, ks = packed.shape[:2]
+    dev = packed.get_device()
+    p = _plain(packed, _U8, (n, ks, 4, 16, 16), "packed", dev)
+    out = _new(packed, (16 * n, 64 * ks), _U8)
+    _on_gpu(dev)
+    _check(LIB.fq_mx_unpack(p, 16 * n, 128 * ks, out.data_ptr(), _stream_handle()))
+    return out
+
+
+def _mx_weights(w: torch.Tensor, scales: torch.Tensor, K: int, dev: int) -> Tuple[int, int, int]:
+    """(N, address of packed weights, of their scales)."""
+    n = w.shape[0]
+    return 16 * n, _plain(w, _U8, (n, K // 128, 4, 16, 16), "w_packed", dev), _plain(scales, _U8, (K // 128, 16 * n, 4), "w_scales", dev)
+
+
+def _mx_result(out, like, M, N, bias, dev):
+    bias_at = _weight(bias, N, "bias", dev) or None
+    if out is None:
+        out = _new(like, (M, N), _BF16)
+        return out, out.data_ptr(), N, bias_at
+    return (out, *_matrix(out, _BF16, (M, N), "out", dev), bias_at)
+
+
+def mx_gemm_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(LIB.fq_mx_gemm_workspace_bytes(M, N, K))
+
+
+def mx_gemm(a_codes: torch.Tensor, a_scales: torch.Tensor, w_packed: torch.Tensor, w_scales: torch.Tensor,
+            bias: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Product of microscaled tokens [M, K] and packed weights [N, K] (mx_pack), plus bias fp32 [N]: bf16 [M, N]."""
+    dev = a_codes.get_device()
+    M, K, a, sa = _mx_codes(a_codes, a_scales, "a_codes", dev)
+    N, w, sw = _mx_weights(w_packed, w_scales, K, dev)
+    out, y, ldy, bias_at = _mx_result(out, a_codes, M, N, bias, dev)
+    _on_gpu(dev)
+    if ws is None:
+        ws = _scratch(LIB.fq_mx_gemm_workspace_bytes(M, N, K), a_codes.device)
+    room, size = _room(ws, dev)
+    rc = LIB.fq_mx_gemm(a, sa, w, sw, bias_at, y, ldy, M, N, K, room, size, _stream_handle())
+    if rc:
+        _check(rc)
+    return out
+
+
+def mx_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(LIB.fq_mx_linear_workspace_bytes(M, N, K))
+
+
+def mx_linear(x: torch.Tensor, w_packed: torch.Tensor, w_scales: torch.Tensor, b: int = 1, smooth_inv: Optional[torch.Tensor] = None,
+              post_inv: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """mx_quant of bf16 x [M, K], then mx_gemm: bf16 [M, N]."""
+    M, K = x.shape
+    dev = x.get_device()
+    at, ld = _matrix(x, _BF16, (M, K), "x", dev)
+    N, w, sw = _mx_weights(w_packed, w_scales, K, dev)
+    pre, post = _weight(smooth_inv, K, "smooth_inv", dev) or None, _weight(post_inv, K, "post_inv", dev) or None
+    out, y, ldy, bias_at = _mx_result(out, x, M, N, bias, dev)
+    _on_gpu(dev)
+    if ws is None:
+        ws = _scratch(LIB.fq_mx_linear_workspace_bytes(M, N, K), x.device)
+    room, size = _room(ws, dev)
+    rc = LIB.fq_mx_linear(at, ld, pre, post, M, K, N, b, w, sw, bias_at, y, ldy, room, size, _stream_handle())
+    if rc:
+        _check(rc)
+    return out
+
+
+class MXLinear:
+    """One projection with microscaled weights: w fp32 [N, K] folded, rounded and packed, kept on the device."""
+
+    def __init__(self, w: torch.Tensor, b: int = 1, col_scale: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                 post_scale: Optional[torch.Tensor] = None):
+        self.N, self.K = w.shape
+        self.b, self.bias = b, bias
+        codes, self.w_scales = mx_quant(w, b, col_scale, post_scale)
+        self.w_packed = mx_pack(codes)
+
+    def __call__(self, x: torch.Tensor, smooth_inv: Optional[torch.Tensor] = None, post_inv: Optional[torch.Tensor] = None,
+                 ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        return mx_linear(x, self.w_packed, self.w_scales, self.b, smooth_inv, post_inv, self.bias, ws, out)
+
+    def product(self, codes: torch.Tensor, scales: torch.Tensor, ws: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The product alone, for tokens that norm_mx_quant or mx_quant rounded (several projections of one site)."""
+        return mx_gemm(codes, scales, self.w_packed, self.w_scales, self.bias, ws, out)
