@@ -160,6 +160,30 @@ __device__ __forceinline__ void lds_write16_untracked(void *p, uint4 v) {
   asm volatile("ds_write_b128 %0, %1" ::"v"(a), "v"(w) : "memory");
 }
 
+// 16 bytes per lane from a buffer straight into LDS (lane l -> dst + 16 l).
+__device__ __forceinline__ void buffer_to_lds16(__amdgpu_buffer_rsrc_t r, uint32_t voff, uint32_t soff, void *dst) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)dst, 16, voff, soff, 0, 0);
+#else
+  (void)r; (void)voff; (void)soff; (void)dst;
+#endif
+}
+
+// Tile (tm, tn) of a workgroup.  The hardware hands workgroup p to XCD p % 8;
+// consecutive logical ids go to one XCD, and ids run down kGroup row tiles before the next
+// column tile, so the tiles an XCD works on at a time form a near-square block whose rows and
+// columns its L2 serves repeatedly.
+constexpr int kGroup = 4;
+__device__ __forceinline__ void tile_of(int lin, int total, int ntm, int ntn, int &tm, int &tn) {
+  const int x = lin & 7, q = total >> 3, r = total & 7;
+  const int id = x * q + min(x, r) + (lin >> 3);
+  const int grp = id / (kGroup * ntn);
+  const int inner = id - grp * kGroup * ntn;
+  const int gm = min(kGroup, ntm - grp * kGroup);
+  tn = inner / gm;
+  tm = grp * kGroup + (inner - tn * gm);
+}
+
 // s_waitcnt vmcnt(n) leaving the other counters alone (gfx9 encoding)
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() {

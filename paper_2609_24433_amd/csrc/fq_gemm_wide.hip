@@ -20,30 +20,6 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 
 constexpr int kBN = 128;  // columns of an output tile (256 rows)
 
-// 16 bytes per lane from a buffer straight into LDS (lane l -> dst + 16 l).
-__device__ __forceinline__ void buffer_to_lds16(__amdgpu_buffer_rsrc_t r, uint32_t voff, uint32_t soff, void *dst) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)dst, 16, voff, soff, 0, 0);
-#else
-  (void)r; (void)voff; (void)soff; (void)dst;
-#endif
-}
-
-// Tile (tm, tn) of a workgroup.  The hardware hands workgroup p to XCD p % 8;
-// consecutive logical ids go to one XCD, and ids run down kGroup row tiles before the next
-// column tile, so the tiles an XCD works on at a time form a near-square block whose rows and
-// columns its L2 serves repeatedly.
-constexpr int kGroup = 4;
-__device__ __forceinline__ void tile_of(int lin, int total, int ntm, int ntn, int &tm, int &tn) {
-  const int x = lin & 7, q = total >> 3, r = total & 7;
-  const int id = x * q + min(x, r) + (lin >> 3);
-  const int grp = id / (kGroup * ntn);
-  const int inner = id - grp * kGroup * ntn;
-  const int gm = min(kGroup, ntm - grp * kGroup);
-  tn = inner / gm;
-  tm = grp * kGroup + (inner - tn * gm);
-}
-
 // A wave's 32 TI x 32 TJ part (rows rw, columns cw of the workgroup's tile) of the output.  Lane
 // l holds column l % 32 and rows 8 (e / 4) + 4 (l / 32) + e % 4 of each 32 x 32 tile; `sums`
 // gives the exact integer sum of (i, j, e).  The wave rescales, stages its bf16 rows in its own

@@ -1,5 +1,8 @@
 // Product of microscaled 4-bit codes: y = bf16(sum over blocks 2^(ea + ew - 254) sum a w + bias) on the
 // matrix instructions that take E2M1 operands with a scale byte per lane.
+#include <cmath>
+
+#include "fq_f6.hpp"
 #include "fq_launch.hpp"
 #include "fq_mx.hpp"
 
@@ -7,8 +10,10 @@ namespace fq {
 
 namespace {
 
-typedef int v8i __attribute__((ext_vector_type(8)));
-typedef float v4f __attribute__((ext_vector_type(4)));
+constexpr int kUnits = 256;  // compute units
+
+// Steps of 256 channels, the last of which may have 128.
+inline int steps_of(int K) { return (K / kTileK + 1) / 2; }
 
 // 16 x 16 x 128: lane l holds row (or column) l % 16 and block l / 16, 32 codes in four words (a format
 // selector of 4 is E2M1), its scale in the low byte of sa (sb).
@@ -21,58 +26,550 @@ __device__ __forceinline__ v4f mfma_mx_16(const v4i &a, int sa, const v4i &b, in
 #endif
 }
 
-// One wave per 16 columns and 16 MT rows, operands straight from memory.
-template <int MT>
-__global__ __launch_bounds__(256) void mx_gemm_rows_kernel(MxGemmArgs p) {
-  const int lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
-  const uint32_t cols = (uint32_t)((p.N / 16 + 3) / 4), rb = blockIdx.x / cols;
-  const int64_t nb = (int64_t)(blockIdx.x - rb * cols) * 4 + (threadIdx.x >> 6);
-  if (nb * 16 >= p.N) return;
-  const int ktot = p.K / kTileK;
-  const int64_t m0 = (int64_t)rb * 16 * MT;
-  const uint8_t *w = p.w + nb * ktot * 1024 + lane * 16;
-  const uint32_t *ws = reinterpret_cast<const uint32_t *>(p.w_scale) + nb * 16 + r16;
-  const uint8_t *a[MT];
-  const uint32_t *as[MT];
+// Few rows: the stream of the weights.  A workgroup has 16 NC columns and 16 MT rows; its NW waves share out the steps of
+// 128 channels, every load of a batch of U steps asked for before the batch ahead of it is multiplied, and their sums meet
+// in LDS.  Weights as the left operand: a lane comes to hold four adjacent columns of one row.
+template <int MT, int NC, int NW>
+__global__ __launch_bounds__(64 * NW) void mx_gemm_stream_kernel(MxGemmArgs p) {
+  constexpr int U = MT * NC >= 4 ? 2 : 4;
+  extern __shared__ __attribute__((aligned(16))) float4 sums[];
+  const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t cols = (uint32_t)((p.N / 16 + NC - 1) / NC), rb = blockIdx.x / cols;
+  const int64_t n0 = (int64_t)(blockIdx.x - rb * cols) * 16 * NC, m0 = (int64_t)rb * 16 * MT;
+  const int ktot = p.K / kTileK, per = (ktot + NW - 1) / NW;
+  const int k0 = wave * per, k1 = min(k0 + per, ktot);
+
+  const uint8_t *w[NC], *a[MT];
+  const uint32_t *ws[NC], *as[MT];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int64_t n = n0 + 16 * c < p.N ? n0 + 16 * c : p.N - 16;
+    w[c] = p.w + n / 16 * ktot * 1024 + lane * 16;
+    ws[c] = reinterpret_cast<const uint32_t *>(p.w_scale) + n + r16;
+  }
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     const int64_t row = m0 + 16 * t + r16 < p.M ? m0 + 16 * t + r16 : p.M - 1;
     a[t] = p.a + row * (p.K / 2) + g * 16;
     as[t] = reinterpret_cast<const uint32_t *>(p.a_scale) + row;
   }
-  v4f acc[MT];
+  struct Step {
+    v4i w[NC], a[MT];
+    uint32_t ws[NC], as[MT];
+  };
+  auto load = [&](Step (&b)[U], int k) {
 #pragma unroll
-  for (int t = 0; t < MT; ++t) acc[t] = v4f{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-  for (int ks = 0; ks < ktot; ++ks) {
-    const v4i b = *reinterpret_cast<const v4i *>(w + (int64_t)ks * 1024);
-    const int sb = (int)(ws[(int64_t)ks * p.N] >> (8 * g));
+    for (int i = 0; i < U; ++i) {
+      const int64_t ks = min(k + i, ktot - 1);
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-      const v4i x = *reinterpret_cast<const v4i *>(a[t] + ks * 64);
-      acc[t] = mfma_mx_16(x, (int)(as[t][(int64_t)ks * p.M] >> (8 * g)), b, sb, acc[t]);
+      for (int c = 0; c < NC; ++c) {
+        b[i].w[c] = *reinterpret_cast<const v4i *>(w[c] + ks * 1024);
+        b[i].ws[c] = ws[c][ks * p.N];
+      }
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        b[i].a[t] = *reinterpret_cast<const v4i *>(a[t] + ks * 64);
+        b[i].as[t] = as[t][ks * p.M];
+      }
     }
-  }
-  const float bias = p.bias ? p.bias[nb * 16 + r16] : 0.0f;
+  };
+  v4f acc[MT][NC];
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t m = m0 + 16 * t + 4 * g + i;
-      if (m < p.M) p.y[m * p.ldy + nb * 16 + r16] = (uint16_t)f32_to_bf16(acc[t][i] + bias);
+    for (int c = 0; c < NC; ++c) acc[t][c] = v4f{0.f, 0.f, 0.f, 0.f};
+  auto multiply = [&](const Step (&b)[U], int k) {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (k + i < k1) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+            acc[t][c] = mfma_mx_16(b[i].w[c], (int)(b[i].ws[c] >> (8 * g)), b[i].a[t], (int)(b[i].as[t] >> (8 * g)), acc[t][c]);
+      }
+  };
+  Step x[U], y[U];
+  load(x, k0);
+  for (int k = k0; k < k1; k += 2 * U) {
+    if (k + U < k1) load(y, k + U);
+    multiply(x, k);
+    if (k + 2 * U < k1) load(x, k + 2 * U);
+    multiply(y, k + U);
+  }
+
+  // every wave's sums side by side; each lane's four columns of one row are added up in the order of the waves
+  constexpr int TILES = MT * NC;
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      sums[(wave * TILES + t * NC + c) * 64 + lane] = make_float4(acc[t][c][0], acc[t][c][1], acc[t][c][2], acc[t][c][3]);
+  __syncthreads();
+  for (int tile = wave; tile < TILES; tile += NW) {
+    float4 v = sums[tile * 64 + lane];
+#pragma unroll
+    for (int s = 1; s < NW; ++s) {
+      const float4 x4 = sums[(s * TILES + tile) * 64 + lane];
+      v.x += x4.x;
+      v.y += x4.y;
+      v.z += x4.z;
+      v.w += x4.w;
     }
+    const int t = tile / NC, c = tile - t * NC;
+    const int64_t m = m0 + 16 * t + r16, n = n0 + 16 * c + 4 * g;
+    if (m >= p.M || n >= p.N) continue;
+    if (p.bias) {
+      const float4 b = *reinterpret_cast<const float4 *>(p.bias + n);
+      v.x += b.x;
+      v.y += b.y;
+      v.z += b.z;
+      v.w += b.w;
+    }
+    *reinterpret_cast<uint2 *>(p.y + m * p.ldy + n) =
+        make_uint2(f32_to_bf16(v.x) | (f32_to_bf16(v.y) << 16), f32_to_bf16(v.z) | (f32_to_bf16(v.w) << 16));
+  }
+}
+
+// 32 x 32 x 64: lane l holds row (or column) l % 32 and block l / 32; its scale is byte SEL of sa (sb).
+template <int SEL>
+__device__ __forceinline__ v16f mfma_mx_32(const v4i &a, int sa, const v4i &b, int sb, v16f c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(v8i{a.x, a.y, a.z, a.w, 0, 0, 0, 0},
+                                                         v8i{b.x, b.y, b.z, b.w, 0, 0, 0, 0}, c, 4, 4, SEL, sa, SEL, sb);
+#else
+  return c;
+#endif
+}
+
+__device__ __forceinline__ void buffer_to_lds4(__amdgpu_buffer_rsrc_t r, uint32_t voff, void *dst) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)dst, 4, voff, 0, 0, 0);
+#else
+  (void)r; (void)voff; (void)dst;
+#endif
+}
+
+struct TileParams {
+  MxGemmArgs g;
+  float *partial;   // [splits][M][N], or NULL
+  int tiles, ntm, ntn, splits;
+  int steps;        // steps of 256 channels of a slice of K (the last slice may have fewer)
+};
+
+template <int TI, int TJ, int WM, int WN, int STAGES>
+struct TileShape {
+  static constexpr int NW = WM * WN, BM = 32 * TI * WM, BN = 32 * TJ * WN;
+  static constexpr int A = BM * 128, B = BN * 128, S = (BM + BN) * 8, STAGE = A + B + S;
+  static constexpr int STRIDE = 64 * TJ + 16;                       // bytes of a staged output row
+  static constexpr int LDS = STAGES * STAGE + NW * 16 * STRIDE;
+  static constexpr int IA = A / 1024 / NW, IB = B / 1024 / NW, IS_ALL = S / 256, IS = (IS_ALL + NW - 1) / NW;
+  static constexpr int LPS = IA + IB + IS;
+  static_assert(IA * NW * 1024 == A && IB * NW * 1024 == B && BM % 64 == 0 && BN % 64 == 0, "whole loads");
+};
+
+// What a workgroup works on: an output tile and a piece of K, in steps of 256 channels from `first` up to `last`.
+struct Piece {
+  int64_t m0, n0;
+  int rows, cols, first, last, split;
+};
+
+// Workgroups take pieces blockIdx, blockIdx + gridDim, .. and read them as one stream of steps through a ring in LDS:
+// the next piece's first steps arrive while the last ones of this are multiplied and its outputs stored.
+template <int TI, int TJ, int WM, int WN, int STAGES, bool SPLIT>
+__global__ __launch_bounds__(64 * WM * WN) void mx_gemm_tile_kernel(TileParams p) {
+  using T = TileShape<TI, TJ, WM, WN, STAGES>;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int K = p.g.K, ktot = K / kTileK, steps_all = (ktot + 1) / 2, total = p.tiles * p.splits;
+  auto piece_of = [&](int lin) {
+    Piece c;
+    c.split = __builtin_amdgcn_readfirstlane(lin / p.tiles);
+    int tm, tn;
+    tile_of(lin - c.split * p.tiles, p.tiles, p.ntm, p.ntn, tm, tn);
+    c.m0 = (int64_t)__builtin_amdgcn_readfirstlane(tm) * T::BM;
+    c.n0 = (int64_t)__builtin_amdgcn_readfirstlane(tn) * T::BN;
+    c.rows = min((int)p.g.M - (int)c.m0, T::BM);
+    c.cols = min((int)p.g.N - (int)c.n0, T::BN);
+    c.first = c.split * p.steps;
+    c.last = min(c.first + p.steps, steps_all);
+    return c;
+  };
+
+  // Ring loads of one step: rows in KBs of 8 rows x 128 bytes, their 16-byte pieces exchanged by (row >> 1) & 7; weight
+  // tiles as they lie; scale words of both halves of the step, rows then columns.  What lies behind the
+  // matrices comes back as zeros.  Where K ends inside a step, the second half's codes are others' (finite, as all
+  // codes) and its scale bytes are made zeros: products of 2^-254, which vanish.
+  // (offsets of a load are added up where it goes out: held in registers they cost 8 and more)
+  uint32_t avoff[2], lane16 = lane * 16u;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = (wave * T::IA + i) * 8 + (lane >> 3);
+    avoff[i] = (uint32_t)row * (uint32_t)(K / 2) + ((lane & 7) ^ ((row >> 1) & 7)) * 16u;
+  }
+
+  // The step that is loaded next: it walks through this workgroup's pieces, and comes to read empty buffers.
+  const int64_t msteps = p.g.M * 4, nsteps = p.g.N * 4;  // bytes of a step's scale words
+  Piece from = piece_of(blockIdx.x);
+  int from_lin = blockIdx.x, from_step = from.first, a_bytes, w_bytes;
+  const uint8_t *from_a, *from_w, *from_sa, *from_sw;
+  auto turn = [&] {
+    from_a = p.g.a + from.m0 * (K / 2);
+    from_w = p.g.w + from.n0 / 16 * ktot * 1024;
+    from_sa = p.g.a_scale + 2 * from.first * msteps + from.m0 * 4;
+    from_sw = p.g.w_scale + 2 * from.first * nsteps + from.n0 * 4;
+    a_bytes = from.rows * (K / 2);
+    w_bytes = from.cols / 16 * ktot * 1024;
+  };
+  turn();
+  auto advance = [&] {
+    from_sa += 2 * msteps;
+    from_sw += 2 * nsteps;
+    if (++from_step < from.last) return;
+    from_lin += gridDim.x;
+    if (from_lin < total) {
+      from = piece_of(from_lin);
+      from_step = from.first;
+      turn();
+    } else {
+      from.rows = from.cols = a_bytes = w_bytes = 0;
+    }
+  };
+  auto issue = [&](int slot, int q) {
+    uint8_t *st = lds + slot * T::STAGE;
+    if (q < T::IA) {
+      buffer_to_lds16(buffer_of(from_a, a_bytes), avoff[q & 1] + (uint32_t)(q >> 1) * 8u * (uint32_t)K, (uint32_t)from_step * 128u,
+                      st + (wave * T::IA + q) * 1024);
+    } else if (q < T::IA + T::IB) {
+      const int kb = wave * T::IB + q - T::IA;
+      buffer_to_lds16(buffer_of(from_w, w_bytes), lane16 + (uint32_t)(kb >> 1) * (uint32_t)ktot * 1024u + (kb & 1) * 1024u,
+                      (uint32_t)from_step * 2048u, st + T::A + kb * 1024);
+    } else {
+      const int idx = min(wave * T::IS + q - T::IA - T::IB, T::IS_ALL - 1);
+      const bool is_b = idx >= T::BM / 32;
+      const int j = is_b ? idx - T::BM / 32 : idx, per = (is_b ? T::BN : T::BM) / 64;
+      const int h = j >= per ? 1 : 0, part = j - h * per;
+      const uint8_t *src = (is_b ? from_sw : from_sa) + (h ? (is_b ? nsteps : msteps) : 0);
+      const int bytes = 2 * from_step + h < ktot ? 4 * (is_b ? from.cols : from.rows) : 0;
+      buffer_to_lds4(buffer_of(src, bytes), (lane16 >> 2) + (uint32_t)part * 256u, st + T::A + T::B + idx * 256);
+    }
+  };
+
+  // Operands of chunk q (64 channels): lane l takes row (or column) l % 32 and block 2 q + l / 32; its scale is byte
+  // 2 (q % 2) of the word of half q / 2, shifted by l / 32 bytes.
+  const int u = lane >> 5, r32 = lane & 31;
+  const int wm = wave / WN, wn = wave - wm * WN;
+  const int arow = wm * 32 * TI + r32;
+  int abase = arow * 128 + ((u ^ ((r32 >> 1) & 7)) * 16);
+  int bbase = T::A + wn * TJ * 4096 + (r32 >> 4) * 2048 + u * 256 + (r32 & 15) * 16;
+  int sabase = T::A + T::B + arow * 4, sbbase = T::A + T::B + T::BM * 8 + (wn * 32 * TJ + r32) * 4;
+  v4i ra[2][TI], rb[2][TJ];
+  int sa[2][TI], sb[2][TJ];
+  constexpr int NRD = TI + TJ;
+  auto read = [&](int set, int slot, int q, int r) {  // in the order the products want them
+    const uint8_t *st = lds + slot * T::STAGE;
+    if (r >= 1 && r <= TI) {
+      ra[set][r - 1] = *reinterpret_cast<const v4i *>(st + (abase ^ (q * 32)) + (r - 1) * 4096);
+      if ((q & 1) == 0) sa[q >> 1][r - 1] = *reinterpret_cast<const int *>(st + sabase + (q >> 1) * T::BM * 4 + (r - 1) * 128);
+    } else {
+      const int j = r == 0 ? 0 : r - TI;
+      rb[set][j] = *reinterpret_cast<const v4i *>(st + bbase + (q >> 1) * 1024 + (q & 1) * 512 + j * 4096);
+      if ((q & 1) == 0) sb[q >> 1][j] = *reinterpret_cast<const int *>(st + sbbase + (q >> 1) * T::BN * 4 + j * 128);
+    }
+  };
+  v16f acc[TI][TJ];
+  auto pin = [&](v16f (&a)[TJ]) {
+    __builtin_amdgcn_sched_barrier(0);
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) asm volatile("" : "+a"(a[j]));
+#endif
+  };
+  auto clear = [&] {
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+      for (int j = 0; j < TJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < TI; ++i) pin(acc[i]);
+  };
+  int there = -1;  // 0: the step's second half lies behind K
+  auto product = [&](auto chunk, int i, int j) {
+    constexpr int q = decltype(chunk)::value;
+    // where a word is first used: its read has landed
+    if (q % 2 == 0 && j == 0) sa[q >> 1][i] = (q ? sa[1][i] & there : sa[0][i]) >> (8 * u);
+    if (q % 2 == 0 && i == 0) sb[q >> 1][j] = (q ? sb[1][j] & there : sb[0][j]) >> (8 * u);
+    acc[i][j] = mfma_mx_32<2 * (q & 1)>(ra[q & 1][i], sa[q >> 1][i], rb[q & 1][j], sb[q >> 1][j], acc[i][j]);
+  };
+
+  // The loads of the step STAGES ahead go out behind the barrier of a step's last chunk, LATE of them in the next
+  // step's first.
+  constexpr int LATE = T::LPS / 2;
+  int slot = 0;
+  auto chunk = [&](auto c, auto end) {
+    constexpr int q = decltype(c)::value;
+    constexpr bool END = decltype(end)::value;
+    const int next = slot == STAGES - 1 ? 0 : slot + 1, prev = slot == 0 ? STAGES - 1 : slot - 1;
+    int r = 0, g = 0;
+#pragma unroll
+    for (int t = 0; t < TI * TJ; ++t) {
+      __builtin_amdgcn_sched_barrier(0);
+      product(c, t % TI, t / TI);
+      __builtin_amdgcn_sched_barrier(0);
+      if (END && t == 0) {
+        // (pinned: the compiler would move this step's products behind the branch in there)
+#pragma unroll
+        for (int i = 0; i < TI; ++i) pin(acc[i]);
+        advance();
+        // every read of this step's slot is done; the next step's loads have landed
+        wait_vmcnt<(STAGES - 2) * T::LPS>();
+        lds_barrier();
+      }
+      constexpr int ROOM = TI * TJ > 1 ? TI * TJ - 1 : 1, PER = (NRD + ROOM - 1) / ROOM;
+#pragma unroll
+      for (int h = 0; h < PER; ++h)
+        if (r < NRD) read((q + 1) & 1, END ? next : slot, END ? 0 : q + 1, r++);
+      constexpr int LPER = (T::LPS - LATE + TI * TJ - 1) / (TI * TJ);
+#pragma unroll
+      for (int h = 0; h < LPER; ++h) {
+        if (q == 0 && g < LATE) issue(prev, T::LPS - LATE + g++);
+        if (END && g < T::LPS - LATE) issue(slot, g++);
+      }
+    }
+    if (END) slot = next;
+  };
+  constexpr std::integral_constant<int, 0> C0{};
+  constexpr std::integral_constant<int, 1> C1{};
+  constexpr std::integral_constant<int, 2> C2{};
+  constexpr std::integral_constant<int, 3> C3{};
+  constexpr std::false_type mid{};
+  constexpr std::true_type end{};
+
+  Piece cur = from;
+#pragma unroll
+  for (int s = 0; s < STAGES; ++s) {
+#pragma unroll
+    for (int q = 0; q < (s == STAGES - 1 ? T::LPS - LATE : T::LPS); ++q) issue(s, q);
+    if (s < STAGES - 1) advance();
+  }
+  wait_vmcnt<(STAGES - 2) * T::LPS + T::LPS - LATE>();
+  lds_barrier();
+#pragma unroll
+  for (int r = 0; r < NRD; ++r) read(0, 0, 0, r);
+
+  clear();
+  for (int lin = blockIdx.x, ks = cur.first;;) {
+#pragma unroll
+    for (int i = 0; i < TI; ++i) pin(acc[i]);
+    // the same sums made in every step, not held in a register each over the loop
+    asm volatile("" : "+v"(avoff[0]), "+v"(avoff[1]), "+v"(lane16), "+v"(abase), "+v"(bbase), "+v"(sabase), "+v"(sbbase));
+    there = 2 * ks + 1 < ktot ? -1 : 0;
+    chunk(C0, mid);
+    chunk(C1, mid);
+    chunk(C2, mid);
+    chunk(C3, end);
+    if (++ks < cur.last) continue;
+
+    // Lane l holds column l % 32 and rows 8 (e / 4) + 4 (l / 32) + e % 4 of each 32 x 32 tile.
+    int el = lane;
+    asm volatile("" : "+v"(el));  // keeps the addresses below out of the loop's registers
+    const int eu = el >> 5, e32 = el & 31;
+    const int rw = wm * 32 * TI, cw = wn * 32 * TJ;
+    if constexpr (SPLIT) {
+      float *out = p.partial + (int64_t)cur.split * p.g.M * p.g.N;
+#pragma unroll
+      for (int i = 0; i < TI; ++i) {
+        pin(acc[i]);
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int m = rw + 32 * i + 8 * (e >> 2) + 4 * eu + (e & 3), n = cw + 32 * j + e32;
+            if (m < cur.rows && n < cur.cols) out[(cur.m0 + m) * p.g.N + cur.n0 + n] = acc[i][j][e];
+          }
+      }
+    } else {
+      // bf16 rows, 16 at a time, through the wave's own part of LDS, so that they leave in 16-byte pieces
+      constexpr int CPR = 4 * TJ;
+      uint8_t *stage = lds + STAGES * T::STAGE + wave * 16 * T::STRIDE;
+      float bias[TJ];
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) {
+        const int n = cw + 32 * j + e32;
+        bias[j] = p.g.bias && n < cur.cols ? p.g.bias[cur.n0 + n] : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * TI; ++i) {
+        // one group's values at a time in ordinary registers: without the pin the compiler copies all of them at once,
+        // and runs out of registers for the loop
+        if (i % 2 == 0) pin(acc[i / 2]);
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            *reinterpret_cast<uint16_t *>(stage + (4 * eu) * T::STRIDE + e32 * 2 + (8 * (e >> 2) + (e & 3)) * T::STRIDE + 64 * j) =
+                (uint16_t)f32_to_bf16(acc[i / 2][j][8 * (i & 1) + e] + bias[j]);
+        wave_lds_fence();
+#pragma unroll
+        for (int q = 0; q < CPR / 4; ++q) {
+          const int c = q * 64 + el, row = c / CPR, ch = c % CPR;
+          const int m = rw + 16 * i + row, n = cw + ch * 8;
+          if (m < cur.rows && n < cur.cols)
+            *reinterpret_cast<uint4 *>(p.g.y + (cur.m0 + m) * p.g.ldy + cur.n0 + n) =
+                *reinterpret_cast<const uint4 *>(stage + row * T::STRIDE + ch * 16);
+        }
+        wave_lds_fence();
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    lin += gridDim.x;
+    if (lin >= total) break;
+    cur = piece_of(lin);
+    ks = cur.first;
+    clear();
+  }
+  wait_vmcnt<0>();  // the ring's trailing loads are over before LDS is given back
+}
+
+// The slices' sums, the bias and the rounding.
+__global__ __launch_bounds__(256) void mx_join_kernel(const float *partial, int splits, const float *bias, uint16_t *y, int64_t ldy,
+                                                      int64_t M, int64_t N) {
+  const int64_t per = N / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= M * per) return;
+  const int64_t m = i / per, n = (i - m * per) * 8;
+  float v[8] = {};
+  for (int s = 0; s < splits; ++s) {
+    const float4 *f = reinterpret_cast<const float4 *>(partial + ((int64_t)s * M + m) * N + n);
+    const float4 a = f[0], b = f[1];
+    const float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += w[j];
+  }
+  uint32_t o[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (bias) {
+      v[2 * j] += bias[n + 2 * j];
+      v[2 * j + 1] += bias[n + 2 * j + 1];
+    }
+    o[j] = f32_to_bf16(v[2 * j]) | (f32_to_bf16(v[2 * j + 1]) << 16);
+  }
+  *reinterpret_cast<uint4 *>(y + m * ldy + n) = make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+template <int MT, int NC, int NW>
+hipError_t launch_stream(const MxGemmArgs &g, hipStream_t s) {
+  constexpr int LDS = NW * MT * NC * 1024;
+  static_assert(LDS <= 65536, "no attribute needed");
+  const int64_t grid = (g.N / 16 + NC - 1) / NC * ((g.M + 16 * MT - 1) / (16 * MT));
+  hipLaunchKernelGGL((mx_gemm_stream_kernel<MT, NC, NW>), dim3((unsigned)grid), dim3(64 * NW), LDS, s, g);
+  return hipGetLastError();
+}
+
+template <int TI, int TJ, int WM, int WN, int STAGES, bool SPLIT>
+hipError_t launch_tile(TileParams p, hipStream_t s) {
+  using T = TileShape<TI, TJ, WM, WN, STAGES>;
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = allow_dynamic_lds(&mx_gemm_tile_kernel<TI, TJ, WM, WN, STAGES, SPLIT>, T::LDS, done);
+  if (e != hipSuccess) return e;
+  p.ntm = (int)((p.g.M + T::BM - 1) / T::BM);
+  p.ntn = (int)((p.g.N + T::BN - 1) / T::BN);
+  p.tiles = p.ntm * p.ntn;
+  const int64_t total = (int64_t)p.tiles * p.splits;
+  hipLaunchKernelGGL((mx_gemm_tile_kernel<TI, TJ, WM, WN, STAGES, SPLIT>), dim3((unsigned)(total < kUnits ? total : kUnits)), dim3(64 * T::NW),
+                     T::LDS, s, p);
+  return hipGetLastError();
+}
+
+template <int TI, int TJ, int WM, int WN, int STAGES>
+hipError_t launch_tiles(const MxGemmArgs &g, int splits, float *ws, hipStream_t s) {
+  const int steps = steps_of(g.K), per = (steps + splits - 1) / splits;
+  const TileParams p{g, splits > 1 ? ws : nullptr, 0, 0, 0, splits, per};
+  if (splits == 1) return launch_tile<TI, TJ, WM, WN, STAGES, false>(p, s);
+  const hipError_t e = launch_tile<TI, TJ, WM, WN, STAGES, true>(p, s);
+  if (e != hipSuccess) return e;
+  const int64_t blocks = (g.M * (g.N / 8) + 255) / 256;
+  hipLaunchKernelGGL(mx_join_kernel, dim3((unsigned)blocks), dim3(256), 0, s, ws, splits, g.bias, g.y, g.ldy, g.M, g.N);
+  return hipGetLastError();
+}
+
+// The kernels to choose from, and the microseconds that a call takes by what was measured (600 calls of 1 to 2048 rows,
+// K 128 to 16384, N 256 to 32768, in a graph of calls in a row; the formulas are within 10% of a call at the root mean square, and
+// the kernel that they choose takes 1% more than the best of all on average, 16% at most).
+struct StreamKind {
+  int mt, nc, nw;
+  hipError_t (*launch)(const MxGemmArgs &, hipStream_t);
+  // a call, a batch of loads, a workgroup that a compute unit runs, and that one's steps of 128 channels a column tile and a row tile
+  float call, batch, group, column, row;
+};
+const StreamKind kStream[] = {
+    {1, 1, 4, launch_stream<1, 1, 4>, 2.88f, 0.018f, 0.21f, 0.0285f, 0.0f},
+    {1, 1, 8, launch_stream<1, 1, 8>, 2.81f, 0.0f, 0.60f, 0.0246f, 0.0f},
+    {1, 2, 4, launch_stream<1, 2, 4>, 2.94f, 0.016f, 0.38f, 0.0179f, 0.0f},
+    {2, 1, 4, launch_stream<2, 1, 4>, 2.44f, 0.30f, 0.58f, 0.0f, 0.0246f},
+    {2, 2, 8, launch_stream<2, 2, 8>, 2.50f, 0.0f, 0.99f, 0.0355f, 0.0f},
+    {4, 2, 4, launch_stream<4, 2, 4>, 2.77f, 0.006f, 0.80f, 0.0f, 0.0274f},
+};
+struct TileKind {
+  int bm, bn;
+  hipError_t (*launch)(const MxGemmArgs &, int, float *, hipStream_t);
+  // a call, a step of 256 channels alone and with all compute units at work, the outputs of a tile then; a split K's
+  // second kernel, and a million bytes of partial sums
+  float call, step, step_full, outputs, join, partial;
+};
+const TileKind kTiles[] = {
+    {64, 128, launch_tiles<1, 1, 2, 4, 4>, 4.03f, 0.38f, 0.01f, 1.39f, 3.28f, 0.25f},
+    {128, 128, launch_tiles<2, 1, 2, 4, 3>, 4.54f, 0.42f, 0.147f, 1.0f, 3.34f, 0.29f},
+    {128, 256, launch_tiles<2, 2, 2, 4, 2>, 5.45f, 0.72f, 0.31f, 1.06f, 3.87f, 0.277f},
+    {256, 256, launch_tiles<4, 2, 2, 4, 2>, 7.15f, 1.10f, 0.325f, 4.77f, 6.25f, 0.197f},
+};
+
+struct Plan {
+  int stream, tile, splits;  // one of stream and tile is -1
+};
+
+Plan plan_of(int64_t M, int64_t N, int K) {
+  Plan best{0, -1, 1};
+  float least = INFINITY;
+  const int ktot = K / kTileK, steps = steps_of(K);
+  for (int i = 0; i < (int)(sizeof kStream / sizeof kStream[0]); ++i) {
+    const StreamKind &k = kStream[i];
+    const int64_t groups = (N / 16 + k.nc - 1) / k.nc * ((M + 16 * k.mt - 1) / (16 * k.mt));
+    if (groups > 0x7FFFFFFF) continue;
+    const float rounds = (float)((groups + kUnits - 1) / kUnits);
+    const int per = (ktot + k.nw - 1) / k.nw, u = k.mt * k.nc >= 4 ? 2 : 4;
+    const float t = k.call + k.batch * (float)((per + u - 1) / u) + rounds * (k.group + (float)ktot * ((float)k.nc * k.column + (float)k.mt * k.row));
+    if (t < least) least = t, best = Plan{i, -1, 1};
+  }
+  for (int i = 0; i < (int)(sizeof kTiles / sizeof kTiles[0]); ++i) {
+    const TileKind &k = kTiles[i];
+    for (int want = 1; want <= 8 && (want == 1 || steps / want >= 2); want *= 2) {
+      const int per = (steps + want - 1) / want, splits = (steps + per - 1) / per;  // no slice is empty
+      const int64_t pieces = ((M + k.bm - 1) / k.bm) * ((N + k.bn - 1) / k.bn) * splits;
+      if (pieces > 0x7FFFFFFF) continue;
+      const float rounds = (float)((pieces + kUnits - 1) / kUnits), full = (float)pieces / (rounds * (float)kUnits);
+      float t = k.call + rounds * ((float)per * (k.step + k.step_full * full) + k.outputs * full);
+      if (splits > 1) t += k.join + k.partial * (float)splits * (float)M * (float)N * 4e-6f;
+      if (t < least) least = t, best = Plan{-1, i, splits};
+    }
+  }
+  return best;
 }
 
 }  // namespace
 
-size_t mx_gemm_workspace(int64_t, int64_t, int64_t) { return 0; }
+size_t mx_gemm_workspace(int64_t M, int64_t N, int64_t K) {
+  const Plan p = plan_of(M, N, (int)K);
+  return p.splits > 1 ? (size_t)p.splits * (size_t)M * (size_t)N * 4 : 0;
+}
 
-hipError_t launch_mx_gemm(const MxGemmArgs &g, void *, hipStream_t s) {
-  const int rows = g.M <= 16 ? 16 : 64;
-  const int64_t grid = (g.N / 16 + 3) / 4 * ((g.M + rows - 1) / rows);  // at most 2^40 outputs: fits 31 bits
-  if (rows == 16) hipLaunchKernelGGL(mx_gemm_rows_kernel<1>, dim3((unsigned)grid), dim3(256), 0, s, g);
-  else hipLaunchKernelGGL(mx_gemm_rows_kernel<4>, dim3((unsigned)grid), dim3(256), 0, s, g);
-  return hipGetLastError();
+hipError_t launch_mx_gemm(const MxGemmArgs &g, void *ws, hipStream_t s) {
+  const Plan p = plan_of(g.M, g.N, g.K);
+  return p.tile < 0 ? kStream[p.stream].launch(g, s) : kTiles[p.tile].launch(g, p.splits, static_cast<float *>(ws), s);
 }
 
 }  // namespace fq

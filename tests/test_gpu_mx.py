@@ -6,7 +6,7 @@ import torch
 
 from oracle import microscaled as mx
 from tests.gpu_util import DEV, flush
-from tests.mx_util import assert_product, dev, dev_bf16, fq, operands, strided, tokens
+from tests.mx_util import HALF_BF16, assert_product, dev, dev_bf16, fq, operands, strided, tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -118,13 +118,29 @@ def test_product(M, N, K):
     assert torch.equal(fq().mx_gemm(*args), out[:M, :N])  # the same bits again, into rows of another stride
 
 
-@pytest.mark.parametrize("M,N,K", [(300, 512, 512), (513, 784, 1024), (1000, 272, 4096), (700, 2048, 384), (2049, 1040, 256)])
+# every kernel and way of splitting K that the sizes choose: tiles of 64 x 128 to 256 x 256, one a workgroup and several, K
+# ending inside a step, whole and in slices with a short last one
+@pytest.mark.parametrize("M,N,K", [(300, 512, 512), (513, 784, 1024), (1000, 272, 4096), (700, 2048, 384), (2049, 1040, 256),
+                                   (260, 16384, 128), (816, 16384, 640), (2100, 8208, 384), (1500, 4112, 896), (4100, 4112, 1152),
+                                   (300, 256, 16384), (520, 2048, 8320), (816, 2048, 16384), (390, 272, 32768), (260, 1024, 7552),
+                                   (3000, 16384, 2176), (129, 32768, 256)])
 def test_product_of_many_rows(M, N, K):
     flush(f"mx_gemm M={M} N={N} K={K}")
     a, sa = operands(M, K, M)
     w, sw = operands(N, K, N)
-    y = fq().mx_gemm(dev(mx.pack_nibbles(a)), dev(mx.steps(sa)), fq().mx_pack(dev(mx.pack_nibbles(w))), dev(mx.steps(sw)))
-    assert_product(y, mx.decode(a, sa), mx.decode(w, sw))
+    bias = np.random.default_rng(3).standard_normal(N).astype(np.float32) * 100 if M % 2 else None
+    out = torch.full((M + 1, N + 16), 5.0, dtype=torch.bfloat16, device=DEV)
+    args = (dev(mx.pack_nibbles(a)), dev(mx.steps(sa)), fq().mx_pack(dev(mx.pack_nibbles(w))), dev(mx.steps(sw)), None if bias is None else dev(bias))
+    fq().mx_gemm(*args, out=out[:M, :N])
+    av, wv = dev(mx.decode(a, sa)), dev(mx.decode(w, sw))
+    want, size = av @ wv.t(), av.abs() @ wv.abs().t()  # fp64
+    slack = 0.0
+    if bias is not None:
+        want, slack = want + dev(bias).double(), dev(bias).double().abs() * 2.0 ** -22
+    off = (out[:M, :N].double() - want).abs()
+    assert bool((off <= size * 2.0 ** -23 * (K // 32 + 8) + want.abs() * (HALF_BF16 + 2.0 ** -22) + slack).all())
+    assert bool((out[M:] == 5).all()) and bool((out[:, N:] == 5).all())
+    assert torch.equal(fq().mx_gemm(*args), out[:M, :N])
 
 
 @pytest.mark.parametrize("M", [1, 40, 300])
