@@ -750,49 +750,44 @@ def _plain(t: torch.Tensor, dtype, shape, name: str, dev: int) -> int:
     return t.data_ptr()
 
 
+def _matrix(t: torch.Tensor, dtype, shape, name: str, dev: int) -> Tuple[int, int]:
+    """Address and row stride of rows with unit column stride."""
+    ld, step = t.stride()
+    if t.dtype is not dtype or t.shape != shape or (step != 1 and t.numel()):
+        raise ValueError(f"{name}: {str(dtype)[6:]} {list(shape)} with unit column stride")
+    if t.get_device() != dev:
+        raise _elsewhere(name, t, dev)
+    return t.data_ptr(), ld
+
+
 def _new(like: torch.Tensor, shape, dtype) -> torch.Tensor:
     return like.new_empty(shape, dtype=dtype) if type(like) is torch.Tensor else torch.empty(shape, dtype=dtype, device=like.device)
 
 
-def _matrix(t: torch.Tensor, dtype, shape, name: str, dev: int) -> Tuple[int, int]:
-    """Address and row stride of rows with unit column stride."""
-    if t.dtype is not dtype or t.shape != shape or (t.numel() and t.stride(1) != 1):
-        raise ValueError(f"{name}: {str(dtype)[6:]} {list(shape)} with unit column stride")
-    if t.get_device() != dev:
-        raise _elsewhere(name, t, dev)
-    return t.data_ptr(), t.stride(0)
-
-
-def _on_gpu(dev: int) -> None:
-    """The call goes to the current device's current stream, whose kernels see that device's tensors."""
+def _gpu_stream(dev: int) -> int:
+    """The current stream, on which a call's kernels see the current device's tensors only."""
     if dev < 0:
         raise ValueError("the tensors are on the host, not on a GPU")
-    if dev != torch._C._cuda_getDevice():
-        raise ValueError(f"the tensors are on GPU {dev}, the current device is GPU {torch._C._cuda_getDevice()}")
+    here = torch._C._cuda_getDevice()
+    if dev != here:
+        raise ValueError(f"the tensors are on GPU {dev}, the current device is GPU {here}")
+    return torch._C._cuda_getCurrentRawStream(here)
 
 
-def _values_out(out: Optional[torch.Tensor], codes: torch.Tensor, M: int, K: int, dev: int):
-    if out is None:
-        out = _new(codes, (M, K), _BF16)
-        return out, out.data_ptr(), K
-    return (out, *_matrix(out, _BF16, (M, K), "out", dev))
-
-
-def _norm_args(x, weight, residual, sum_out, post_inv):
-    shape = x.shape
-    M, K = shape
-    dev = x.get_device()
-    at, ld = _matrix(x, _BF16, shape, "x", dev)
-    r = ldr = total = lds = 0
-    stream = x
-    if residual is not None:
-        r, ldr = _matrix(residual, _BF16, shape, "residual", dev)
-        stream = _new(x, shape, _BF16) if sum_out is None else sum_out
-        total, lds = (stream.data_ptr(), K) if sum_out is None else _matrix(sum_out, _BF16, shape, "sum_out", dev)
-    elif sum_out is not None:
-        raise ValueError("sum_out needs a residual")
-    return M, K, dev, at, ld, r or None, ldr, _weight(weight, K, "weight", dev) or None, _weight(post_inv, K, "post_inv", dev) or None, \
-        total or None, lds, stream
+def _norm_args(x, weight, residual, sum_out, post_inv, M, K, dev):
+    """The arguments that both norms begin with, and the stream of hidden states after the addition."""
+    at, ld = _matrix(x, _BF16, (M, K), "x", dev)
+    post = None if post_inv is None else _weight(post_inv, K, "post_inv", dev)
+    w = _weight(weight, K, "weight", dev)
+    if residual is None:
+        if sum_out is not None:
+            raise ValueError("sum_out needs a residual")
+        return at, ld, None, 0, w, post, None, 0, x
+    r, ldr = _matrix(residual, _BF16, (M, K), "residual", dev)
+    if sum_out is None:
+        total = _new(x, (M, K), _BF16)
+        return at, ld, r, ldr, w, post, total.data_ptr(), K, total
+    return (at, ld, r, ldr, w, post, *_matrix(sum_out, _BF16, (M, K), "sum_out", dev), sum_out)
 
 
 def norm_quant(x: torch.Tensor, weight: torch.Tensor, b: int, bits: int, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -802,18 +797,17 @@ def norm_quant(x: torch.Tensor, weight: torch.Tensor, b: int, bits: int, residua
     """The residual's addition, the root-mean-square norm with its gain `weight` fp32 [K] and the prologue's rotation and
     rounding, bf16 x, residual [M, K] -> (codes uint8 [M, K*bits/8], delta fp32 [M], the sum bf16 [M, K]; x where there is no
     residual).  sum_out may be x or the residual itself.  The codes are gemm's."""
-    M, K, dev, at, ld, r, ldr, w, post, total, lds, stream = _norm_args(x, weight, residual, sum_out, post_inv)
-    if out_codes is None:
-        out_codes = _new(x, (M, code_bytes(K, bits)), _U8)
-    codes = _plain(out_codes, _U8, (M, code_bytes(K, bits)), "out_codes", dev)
-    if out_delta is None:
-        out_delta = _new(x, (M,), _F32)
-    delta = _plain(out_delta, _F32, (M,), "out_delta", dev)
-    _on_gpu(dev)
-    rc = LIB.fq_norm_quant(at, ld, r, ldr, w, eps, post, M, K, b, bits, clip_ratio, total, lds, codes, delta, _stream_handle())
+    M, K = x.shape
+    dev, width = x.get_device(), K * bits // 8
+    at, ld, r, ldr, w, post, total, lds, states = _norm_args(x, weight, residual, sum_out, post_inv, M, K, dev)
+    codes = _new(x, (M, width), _U8) if out_codes is None else out_codes
+    delta = _new(x, (M,), _F32) if out_delta is None else out_delta
+    c = codes.data_ptr() if out_codes is None else _plain(codes, _U8, (M, width), "out_codes", dev)
+    d = delta.data_ptr() if out_delta is None else _plain(delta, _F32, (M,), "out_delta", dev)
+    rc = LIB.fq_norm_quant(at, ld, r, ldr, w, eps, post, M, K, b, bits, clip_ratio, total, lds, c, d, _gpu_stream(dev))
     if rc:
         _check(rc)
-    return out_codes, out_delta, stream
+    return codes, delta, states
 
 
 def norm_mx_quant(x: torch.Tensor, weight: torch.Tensor, b: int = 1, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -822,37 +816,50 @@ def norm_mx_quant(x: torch.Tensor, weight: torch.Tensor, b: int = 1, residual: O
                   out_scales: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """norm_quant with microscaled codes: (codes uint8 [M, K/2], scales uint8 [K/128, M, 4], the sum).  The codes are
     mx_gemm's."""
-    M, K, dev, at, ld, r, ldr, w, post, total, lds, stream = _norm_args(x, weight, residual, sum_out, post_inv)
-    out_codes, codes, out_scales, scales = _mx_out(x, M, K, out_codes, out_scales, dev)
-    _on_gpu(dev)
-    rc = LIB.fq_norm_mx_quant(at, ld, r, ldr, w, eps, post, M, K, b, total, lds, codes, scales, _stream_handle())
+    M, K = x.shape
+    dev = x.get_device()
+    at, ld, r, ldr, w, post, total, lds, states = _norm_args(x, weight, residual, sum_out, post_inv, M, K, dev)
+    codes, c, scales, s = _mx_out(x, M, K, out_codes, out_scales, dev)
+    rc = LIB.fq_norm_mx_quant(at, ld, r, ldr, w, eps, post, M, K, b, total, lds, c, s, _gpu_stream(dev))
     if rc:
         _check(rc)
-    return out_codes, out_scales, stream
+    return codes, scales, states
+
+
+def _values_out(out: Optional[torch.Tensor], codes: torch.Tensor, M: int, K: int, dev: int):
+    if out is None:
+        out = _new(codes, (M, K), _BF16)
+        return out, out.data_ptr(), K
+    return (out, *_matrix(out, _BF16, (M, K), "out", dev))
 
 
 def read_codes(codes: torch.Tensor, delta: torch.Tensor, bits: int, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Codes of fwht_quant or norm_quant, uint8 [M, K*bits/8] with delta fp32 [M], as values bf16 [M, K]."""
-    if bits not in (4, 8):
+    if bits != 8 and bits != 4:
         raise ValueError("bits: 4 or 8")
-    M, width = codes.shape
+    shape = codes.shape
+    M, width = shape
     K, dev = width * 8 // bits, codes.get_device()
+    c = _plain(codes, _I8 if codes.dtype is _I8 else _U8, shape, "codes", dev)
+    d = _plain(delta, _F32, (M,), "delta", dev)
     out, at, ld = _values_out(out, codes, M, K, dev)
-    c, d = _plain(codes, codes.dtype if codes.dtype is _I8 else _U8, (M, width), "codes", dev), _plain(delta, _F32, (M,), "delta", dev)
-    _on_gpu(dev)
-    rc = LIB.fq_read_codes(c, d, M, K, bits, at, ld, _stream_handle())
+    rc = LIB.fq_read_codes(c, d, M, K, bits, at, ld, _gpu_stream(dev))
     if rc:
         _check(rc)
     return out
 
 
 def _mx_out(x, M, K, codes, scales, dev):
-    cs, ss = (M, K // 2), (K // 128, M, 4)
+    """Outputs of a microscaled rounding, the caller's or new ones, with their addresses."""
     if codes is None:
-        codes = _new(x, cs, _U8)
+        codes = _new(x, (M, K // 2), _U8)
+        c = codes.data_ptr()
+    else:
+        c = _plain(codes, _U8, (M, K // 2), "out_codes", dev)
     if scales is None:
-        scales = _new(x, ss, _U8)
-    return codes, _plain(codes, _U8, cs, "out_codes", dev), scales, _plain(scales, _U8, ss, "out_scales", dev)
+        scales = _new(x, (K // 128, M, 4), _U8)
+        return codes, c, scales, scales.data_ptr()
+    return codes, c, scales, _plain(scales, _U8, (K // 128, M, 4), "out_scales", dev)
 
 
 def mx_quant(x: torch.Tensor, b: int = 1, pre_mult: Optional[torch.Tensor] = None, post_mult: Optional[torch.Tensor] = None,
@@ -860,23 +867,24 @@ def mx_quant(x: torch.Tensor, b: int = 1, pre_mult: Optional[torch.Tensor] = Non
              out_scales: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Rows bf16 (tokens) or fp32 (weights) [M, K] through the folds and the block Hadamard, rounded to microscaled codes:
     (codes uint8 [M, K/2], scales uint8 [K/128, M, 4]).  Tokens: pre_mult = S^-1, post_mult = P^-1; weights: S and P."""
-    M, K = x.shape
+    shape = x.shape
+    M, K = shape
     dev, f32 = x.get_device(), x.dtype is _F32
-    at, ld = _matrix(x, _F32 if f32 else _BF16, (M, K), "x", dev)
-    pre, post = _weight(pre_mult, K, "pre_mult", dev) or None, _weight(post_mult, K, "post_mult", dev) or None
-    out_codes, codes, out_scales, scales = _mx_out(x, M, K, out_codes, out_scales, dev)
-    _on_gpu(dev)
-    rc = LIB.fq_mx_quant(at, f32, ld, pre, post, M, K, b, codes, scales, _stream_handle())
+    at, ld = _matrix(x, _F32 if f32 else _BF16, shape, "x", dev)
+    pre = None if pre_mult is None else _weight(pre_mult, K, "pre_mult", dev)
+    post = None if post_mult is None else _weight(post_mult, K, "post_mult", dev)
+    codes, c, scales, s = _mx_out(x, M, K, out_codes, out_scales, dev)
+    rc = LIB.fq_mx_quant(at, f32, ld, pre, post, M, K, b, c, s, _gpu_stream(dev))
     if rc:
         _check(rc)
-    return out_codes, out_scales
+    return codes, scales
 
 
 def _mx_codes(codes, scales, name, dev) -> Tuple[int, int, int, int]:
     """(M, K, address of the codes, of the scales) of microscaled rows."""
-    M, half = codes.shape
-    K = 2 * half
-    return M, K, _plain(codes, _U8, (M, half), name, dev), _plain(scales, _U8, (K // 128, M, 4), name + "'s scales", dev)
+    shape = codes.shape
+    M, half = shape
+    return M, 2 * half, _plain(codes, _U8, shape, name, dev), _plain(scales, _U8, (half // 64, M, 4), name + "'s scales", dev)
 
 
 def mx_read(codes: torch.Tensor, scales: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -884,8 +892,7 @@ def mx_read(codes: torch.Tensor, scales: torch.Tensor, out: Optional[torch.Tenso
     dev = codes.get_device()
     M, K, c, s = _mx_codes(codes, scales, "codes", dev)
     out, at, ld = _values_out(out, codes, M, K, dev)
-    _on_gpu(dev)
-    rc = LIB.fq_mx_read(c, s, M, K, at, ld, _stream_handle())
+    rc = LIB.fq_mx_read(c, s, M, K, at, ld, _gpu_stream(dev))
     if rc:
         _check(rc)
     return out
@@ -897,8 +904,7 @@ def mx_pack(codes: torch.Tensor) -> torch.Tensor:
     dev = codes.get_device()
     c = _plain(codes, _U8, (N, half), "codes", dev)
     out = _new(codes, (N // 16, half // 64, 4, 16, 16), _U8)
-    _on_gpu(dev)
-    _check(LIB.fq_mx_pack(c, N, 2 * half, out.data_ptr(), _stream_handle()))
+    _check(LIB.fq_mx_pack(c, N, 2 * half, out.data_ptr(), _gpu_stream(dev)))
     return out
 
 
@@ -908,23 +914,21 @@ def mx_unpack(packed: torch.Tensor) -> torch.Tensor:
     dev = packed.get_device()
     p = _plain(packed, _U8, (n, ks, 4, 16, 16), "packed", dev)
     out = _new(packed, (16 * n, 64 * ks), _U8)
-    _on_gpu(dev)
-    _check(LIB.fq_mx_unpack(p, 16 * n, 128 * ks, out.data_ptr(), _stream_handle()))
+    _check(LIB.fq_mx_unpack(p, 16 * n, 128 * ks, out.data_ptr(), _gpu_stream(dev)))
     return out
 
 
-def _mx_weights(w: torch.Tensor, scales: torch.Tensor, K: int, dev: int) -> Tuple[int, int, int]:
-    """(N, address of packed weights, of their scales)."""
+def _mx_operands(w: torch.Tensor, scales: torch.Tensor, bias, out, like, M: int, K: int, dev: int):
+    """(N, addresses of packed weights, their scales and the bias, the output, its address and row stride)."""
     n = w.shape[0]
-    return 16 * n, _plain(w, _U8, (n, K // 128, 4, 16, 16), "w_packed", dev), _plain(scales, _U8, (K // 128, 16 * n, 4), "w_scales", dev)
-
-
-def _mx_result(out, like, M, N, bias, dev):
-    bias_at = _weight(bias, N, "bias", dev) or None
+    N = 16 * n
+    at = _plain(w, _U8, (n, K // 128, 4, 16, 16), "w_packed", dev)
+    s = _plain(scales, _U8, (K // 128, N, 4), "w_scales", dev)
+    b = None if bias is None else _weight(bias, N, "bias", dev)
     if out is None:
         out = _new(like, (M, N), _BF16)
-        return out, out.data_ptr(), N, bias_at
-    return (out, *_matrix(out, _BF16, (M, N), "out", dev), bias_at)
+        return N, at, s, b, out, out.data_ptr(), N
+    return (N, at, s, b, out, *_matrix(out, _BF16, (M, N), "out", dev))
 
 
 def mx_gemm_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -936,13 +940,12 @@ def mx_gemm(a_codes: torch.Tensor, a_scales: torch.Tensor, w_packed: torch.Tenso
     """Product of microscaled tokens [M, K] and packed weights [N, K] (mx_pack), plus bias fp32 [N]: bf16 [M, N]."""
     dev = a_codes.get_device()
     M, K, a, sa = _mx_codes(a_codes, a_scales, "a_codes", dev)
-    N, w, sw = _mx_weights(w_packed, w_scales, K, dev)
-    out, y, ldy, bias_at = _mx_result(out, a_codes, M, N, bias, dev)
-    _on_gpu(dev)
+    N, w, sw, b, out, y, ldy = _mx_operands(w_packed, w_scales, bias, out, a_codes, M, K, dev)
+    stream = _gpu_stream(dev)
     if ws is None:
         ws = _scratch(LIB.fq_mx_gemm_workspace_bytes(M, N, K), a_codes.device)
     room, size = _room(ws, dev)
-    rc = LIB.fq_mx_gemm(a, sa, w, sw, bias_at, y, ldy, M, N, K, room, size, _stream_handle())
+    rc = LIB.fq_mx_gemm(a, sa, w, sw, b, y, ldy, M, N, K, room, size, stream)
     if rc:
         _check(rc)
     return out
@@ -956,17 +959,18 @@ def mx_linear(x: torch.Tensor, w_packed: torch.Tensor, w_scales: torch.Tensor, b
               post_inv: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
               out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """mx_quant of bf16 x [M, K], then mx_gemm: bf16 [M, N]."""
-    M, K = x.shape
+    shape = x.shape
+    M, K = shape
     dev = x.get_device()
-    at, ld = _matrix(x, _BF16, (M, K), "x", dev)
-    N, w, sw = _mx_weights(w_packed, w_scales, K, dev)
-    pre, post = _weight(smooth_inv, K, "smooth_inv", dev) or None, _weight(post_inv, K, "post_inv", dev) or None
-    out, y, ldy, bias_at = _mx_result(out, x, M, N, bias, dev)
-    _on_gpu(dev)
+    at, ld = _matrix(x, _BF16, shape, "x", dev)
+    pre = None if smooth_inv is None else _weight(smooth_inv, K, "smooth_inv", dev)
+    post = None if post_inv is None else _weight(post_inv, K, "post_inv", dev)
+    N, w, sw, bias_at, out, y, ldy = _mx_operands(w_packed, w_scales, bias, out, x, M, K, dev)
+    stream = _gpu_stream(dev)
     if ws is None:
         ws = _scratch(LIB.fq_mx_linear_workspace_bytes(M, N, K), x.device)
     room, size = _room(ws, dev)
-    rc = LIB.fq_mx_linear(at, ld, pre, post, M, K, N, b, w, sw, bias_at, y, ldy, room, size, _stream_handle())
+    rc = LIB.fq_mx_linear(at, ld, pre, post, M, K, N, b, w, sw, bias_at, y, ldy, room, size, stream)
     if rc:
         _check(rc)
     return out

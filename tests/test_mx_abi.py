@@ -161,3 +161,11 @@ def test_a_sum_needs_a_residual():
     t = tensors()
     with pytest.raises(ValueError, match="residual"):
         fq.norm_quant(t["x"], t["weight"], 64, 8, sum_out=t["res"])
+
+
+def test_another_device_than_the_current_one_is_refused(monkeypatch):
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 77, raising=False)
+    assert fq._gpu_stream(0) == 77
+    with pytest.raises(ValueError, match="GPU 1, the current device is GPU 0"):
+        fq._gpu_stream(1)
