@@ -15,92 +15,119 @@ constexpr int kUnits = 256;  // compute units
 // Steps of 256 channels, the last of which may have 128.
 inline int steps_of(int K) { return (K / kTileK + 1) / 2; }
 
-// 16 x 16 x 128: lane l holds row (or column) l % 16 and block l / 16, 32 codes in four words (a format
-// selector of 4 is E2M1), its scale in the low byte of sa (sb).
+// 16 x 16 x 128: lane l holds row (or column) l % 16 and one block of 32 codes in four words (a format selector of 4 is
+// E2M1), any four blocks in the four lane groups as long as both operands have the same; the block's scale is byte SEL
+// of sa (sb).
+template <int SEL>
 __device__ __forceinline__ v4f mfma_mx_16(const v4i &a, int sa, const v4i &b, int sb, v4f c) {
 #if defined(__HIP_DEVICE_COMPILE__)
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v8i{a.x, a.y, a.z, a.w, 0, 0, 0, 0},
-                                                          v8i{b.x, b.y, b.z, b.w, 0, 0, 0, 0}, c, 4, 4, 0, sa, 0, sb);
+                                                          v8i{b.x, b.y, b.z, b.w, 0, 0, 0, 0}, c, 4, 4, SEL, sa, SEL, sb);
 #else
   return c;
 #endif
 }
 
-// Few rows: the stream of the weights.  A workgroup has 16 NC columns and 16 MT rows; its NW waves share out the steps of
-// 128 channels, every load of a batch of U steps asked for before the batch ahead of it is multiplied, and their sums meet
-// in LDS.  Weights as the left operand: a lane comes to hold four adjacent columns of one row.
+// Few rows: the stream of the weights.  A workgroup has 16 NC columns and 16 MT rows; its NW waves share out K in batches of
+// four steps of 128 channels, ask for every load of a batch before they multiply the one ahead, and their sums meet in LDS.
+//   In product i of a batch lane group g multiplies block i of step g: a lane's four scale bytes are one word, loaded once.
+//   Rows go through the wave's own part of LDS: loaded in operand order (a lane a row) they come at 37 bytes a ns and compute
+//   unit, four lanes a row at 120.  Weights are packed in operand order.
+//   Weights are the left operand, so that a lane comes to hold four adjacent columns of one row.
 template <int MT, int NC, int NW>
 __global__ __launch_bounds__(64 * NW) void mx_gemm_stream_kernel(MxGemmArgs p) {
-  constexpr int U = MT * NC >= 4 ? 2 : 4;
-  extern __shared__ __attribute__((aligned(16))) float4 sums[];
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint32_t cols = (uint32_t)((p.N / 16 + NC - 1) / NC), rb = blockIdx.x / cols;
-  const int64_t n0 = (int64_t)(blockIdx.x - rb * cols) * 16 * NC, m0 = (int64_t)rb * 16 * MT;
-  const int ktot = p.K / kTileK, per = (ktot + NW - 1) / NW;
-  const int k0 = wave * per, k1 = min(k0 + per, ktot);
+  // The row blocks of a column block lie behind each other on one XCD (workgroup i runs on XCD i % 8), whose L2 then has
+  // the weights for all but the first.
+  const uint32_t row_blocks = (uint32_t)((p.M + 16 * MT - 1) / (16 * MT)), group = (blockIdx.x >> 3) / row_blocks;
+  const int64_t n0 = ((int64_t)group * 8 + (blockIdx.x & 7)) * 16 * NC, m0 = (int64_t)((blockIdx.x >> 3) - group * row_blocks) * 16 * MT;
+  if (n0 >= p.N) return;
+  const int rows = min((int)p.M - (int)m0, 16 * MT), cols = min((int)p.N - (int)n0, 16 * NC);
+  const int ktot = p.K / kTileK, per = ((ktot + 4 * NW - 1) / (4 * NW)) * 4;
+  const int k1 = min((wave + 1) * per, ktot);
+  int k0 = wave * per;
 
-  const uint8_t *w[NC], *a[MT];
-  const uint32_t *ws[NC], *as[MT];
+  // A KB of LDS has a step of 16 rows, their four pieces exchanged by (row >> 2) & 3 against bank conflicts.  What lies
+  // behind the rows or columns is not stored.
+  const uint8_t *a0 = p.a + m0 * (p.K / 2), *w0 = p.w + n0 / 16 * ktot * 1024;
+  const int abytes = rows * (p.K / 2), wbytes = cols / 16 * ktot * 1024;
+  const uint32_t avoff = (uint32_t)(lane >> 2) * (uint32_t)(p.K / 2) + ((lane & 3) ^ ((lane >> 4) & 3)) * 16u;
+  const uint32_t wvoff = g * 1024u + r16 * 16u;
+  const uint32_t *sa[MT], *sw[NC];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int64_t n = n0 + 16 * c < p.N ? n0 + 16 * c : p.N - 16;
-    w[c] = p.w + n / 16 * ktot * 1024 + lane * 16;
-    ws[c] = reinterpret_cast<const uint32_t *>(p.w_scale) + n + r16;
-  }
+  for (int t = 0; t < MT; ++t) sa[t] = reinterpret_cast<const uint32_t *>(p.a_scale) + m0 + min(16 * t + r16, rows - 1);
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int64_t row = m0 + 16 * t + r16 < p.M ? m0 + 16 * t + r16 : p.M - 1;
-    a[t] = p.a + row * (p.K / 2) + g * 16;
-    as[t] = reinterpret_cast<const uint32_t *>(p.a_scale) + row;
-  }
-  struct Step {
-    v4i w[NC], a[MT];
-    uint32_t ws[NC], as[MT];
+  for (int c = 0; c < NC; ++c) sw[c] = reinterpret_cast<const uint32_t *>(p.w_scale) + n0 + min(16 * c + r16, cols - 1);
+  struct Batch {
+    v4i w[NC][4];
+    uint32_t sw[NC], sa[MT];
   };
-  auto load = [&](Step (&b)[U], int k) {
+  constexpr int LOADS = 4 * MT + 4 * NC + MT + NC;
+  uint8_t *mine = lds + wave * 2 * MT * 4096;
+  auto load = [&](Batch &b, int buf, int at) {
+    // (a batch behind the wave's share is asked of empty buffers: no branch, so that every wait knows its count)
+    const int k = __builtin_amdgcn_readfirstlane(at), on = k < k1 ? -1 : 0;
+    const __amdgpu_buffer_rsrc_t ar = buffer_of(a0, abytes & on), wr = buffer_of(w0, wbytes & on);
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int64_t ks = min(k + i, ktot - 1);
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        b[i].w[c] = *reinterpret_cast<const v4i *>(w[c] + ks * 1024);
-        b[i].ws[c] = ws[c][ks * p.N];
-      }
+      for (int s = 0; s < 4; ++s)
+        buffer_to_lds16(ar, avoff + (uint32_t)t * 8u * (uint32_t)p.K, (uint32_t)min(k + s, ktot - 1) * 64u, mine + ((buf * MT + t) * 4 + s) * 1024);
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        b[i].a[t] = *reinterpret_cast<const v4i *>(a[t] + ks * 64);
-        b[i].as[t] = as[t][ks * p.M];
-      }
-    }
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        b.w[c][i] = __builtin_amdgcn_raw_buffer_load_b128(wr, wvoff + i * 256u + (uint32_t)c * (uint32_t)ktot * 1024u, (uint32_t)k * 1024u, 0);
+    const int64_t step = min(k + g, ktot - 1);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) b.sw[c] = sw[c][step * p.N];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) b.sa[t] = sa[t][step * p.M];
   };
   v4f acc[MT][NC];
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
     for (int c = 0; c < NC; ++c) acc[t][c] = v4f{0.f, 0.f, 0.f, 0.f};
-  auto multiply = [&](const Step (&b)[U], int k) {
+  auto multiply = [&](const Batch &b, int buf, int k) {
+    // a step behind the wave's share: scales of 2^-127 both, and their products vanish (its codes are other steps')
+    const int on = k + g < k1 ? -1 : 0;
+    auto product = [&](auto which) {
+      constexpr int i = decltype(which)::value;
 #pragma unroll
-    for (int i = 0; i < U; ++i)
-      if (k + i < k1) {
+      for (int t = 0; t < MT; ++t) {
+        const v4i a = *reinterpret_cast<const v4i *>(mine + (buf * MT + t) * 4096 + g * 1024 + r16 * 64 + ((i ^ (r16 >> 2)) * 16));
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-          for (int c = 0; c < NC; ++c)
-            acc[t][c] = mfma_mx_16(b[i].w[c], (int)(b[i].ws[c] >> (8 * g)), b[i].a[t], (int)(b[i].as[t] >> (8 * g)), acc[t][c]);
+        for (int c = 0; c < NC; ++c) acc[t][c] = mfma_mx_16<i>(b.w[c][i], (int)b.sw[c] & on, a, (int)b.sa[t] & on, acc[t][c]);
       }
+    };
+    static_for<4>(product);
   };
-  Step x[U], y[U];
-  load(x, k0);
-  for (int k = k0; k < k1; k += 2 * U) {
-    if (k + U < k1) load(y, k + U);
-    multiply(x, k);
-    if (k + 2 * U < k1) load(x, k + 2 * U);
-    multiply(y, k + U);
+  Batch x, y;
+  load(x, 0, k0);
+  if (per <= 4) {  // a batch a wave
+    wait_vmcnt<0>();
+    multiply(x, 0, k0);
+    k0 = k1;
   }
+  for (int k = k0; k < k1; k += 8) {
+    load(y, 1, k + 4);
+    wait_vmcnt<LOADS>();
+    multiply(x, 0, k);
+    lgkm_wait_all();  // the rows are read before others take their place
+    load(x, 0, k + 8);
+    wait_vmcnt<LOADS>();
+    multiply(y, 1, k + 4);
+    lgkm_wait_all();
+  }
+  wait_vmcnt<0>();  // the trailing loads are over: LDS is reused
 
   // every wave's sums side by side; each lane's four columns of one row are added up in the order of the waves
   constexpr int TILES = MT * NC;
+  float4 *sums = reinterpret_cast<float4 *>(lds);
+  __syncthreads();
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -118,16 +145,16 @@ __global__ __launch_bounds__(64 * NW) void mx_gemm_stream_kernel(MxGemmArgs p) {
       v.w += x4.w;
     }
     const int t = tile / NC, c = tile - t * NC;
-    const int64_t m = m0 + 16 * t + r16, n = n0 + 16 * c + 4 * g;
-    if (m >= p.M || n >= p.N) continue;
+    const int m = 16 * t + r16, n = 16 * c + 4 * g;
+    if (m >= rows || n >= cols) continue;
     if (p.bias) {
-      const float4 b = *reinterpret_cast<const float4 *>(p.bias + n);
+      const float4 b = *reinterpret_cast<const float4 *>(p.bias + n0 + n);
       v.x += b.x;
       v.y += b.y;
       v.z += b.z;
       v.w += b.w;
     }
-    *reinterpret_cast<uint2 *>(p.y + m * p.ldy + n) =
+    *reinterpret_cast<uint2 *>(p.y + (m0 + m) * p.ldy + n0 + n) =
         make_uint2(f32_to_bf16(v.x) | (f32_to_bf16(v.y) << 16), f32_to_bf16(v.z) | (f32_to_bf16(v.w) << 16));
   }
 }
@@ -463,9 +490,11 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const float *partial, int 
 
 template <int MT, int NC, int NW>
 hipError_t launch_stream(const MxGemmArgs &g, hipStream_t s) {
-  constexpr int LDS = NW * MT * NC * 1024;
-  static_assert(LDS <= 65536, "no attribute needed");
-  const int64_t grid = (g.N / 16 + NC - 1) / NC * ((g.M + 16 * MT - 1) / (16 * MT));
+  constexpr int LDS = NW * (8 * MT > MT * NC ? 8 * MT : MT * NC) * 1024;
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = allow_dynamic_lds(&mx_gemm_stream_kernel<MT, NC, NW>, LDS, done);
+  if (e != hipSuccess) return e;
+  const int64_t grid = ((g.N / 16 + NC - 1) / NC + 7) / 8 * 8 * ((g.M + 16 * MT - 1) / (16 * MT));
   hipLaunchKernelGGL((mx_gemm_stream_kernel<MT, NC, NW>), dim3((unsigned)grid), dim3(64 * NW), LDS, s, g);
   return hipGetLastError();
 }
@@ -497,22 +526,24 @@ hipError_t launch_tiles(const MxGemmArgs &g, int splits, float *ws, hipStream_t 
   return hipGetLastError();
 }
 
-// The kernels to choose from, and the microseconds that a call takes by what was measured (600 calls of 1 to 2048 rows,
-// K 128 to 16384, N 256 to 32768, in a graph of calls in a row; the formulas are within 10% of a call at the root mean square, and
-// the kernel that they choose takes 1% more than the best of all on average, 16% at most).
+// The kernels to choose from, and the microseconds that a call takes by what was measured (1400 drawn sizes of 1 to
+// 8191 rows, K 128 to 32768, N 64 to 32768, each with every kernel and split, in a graph of calls in a row; the formulas are within
+// 7% (tiles) to 13% of a call at the root mean square, and the kernel that they choose takes 1.3% more than the best of all on
+// average, 48% at most, for calls of 3 us).
 struct StreamKind {
   int mt, nc, nw;
   hipError_t (*launch)(const MxGemmArgs &, hipStream_t);
-  // a call, a batch of loads, a workgroup that a compute unit runs, and that one's steps of 128 channels a column tile and a row tile
-  float call, batch, group, column, row;
+  // a call, a batch of a wave, a workgroup that a compute unit runs, and a step of 128 channels of all but its first
+  float call, batch, group, step;
 };
 const StreamKind kStream[] = {
-    {1, 1, 4, launch_stream<1, 1, 4>, 2.88f, 0.018f, 0.21f, 0.0285f, 0.0f},
-    {1, 1, 8, launch_stream<1, 1, 8>, 2.81f, 0.0f, 0.60f, 0.0246f, 0.0f},
-    {1, 2, 4, launch_stream<1, 2, 4>, 2.94f, 0.016f, 0.38f, 0.0179f, 0.0f},
-    {2, 1, 4, launch_stream<2, 1, 4>, 2.44f, 0.30f, 0.58f, 0.0f, 0.0246f},
-    {2, 2, 8, launch_stream<2, 2, 8>, 2.50f, 0.0f, 0.99f, 0.0355f, 0.0f},
-    {4, 2, 4, launch_stream<4, 2, 4>, 2.77f, 0.006f, 0.80f, 0.0f, 0.0274f},
+    {1, 1, 2, launch_stream<1, 1, 2>, 2.76f, 0.182f, 0.097f, 0.0248f},
+    {1, 1, 4, launch_stream<1, 1, 4>, 2.65f, 0.273f, 0.216f, 0.0244f},
+    {1, 2, 4, launch_stream<1, 2, 4>, 2.68f, 0.417f, 0.269f, 0.0356f},
+    {2, 1, 2, launch_stream<2, 1, 2>, 2.63f, 0.289f, 0.239f, 0.0365f},
+    {2, 2, 8, launch_stream<2, 2, 8>, 1.08f, 1.338f, 1.800f, 0.0541f},
+    {2, 4, 4, launch_stream<2, 4, 4>, 2.14f, 1.063f, 0.948f, 0.0733f},
+    {4, 4, 4, launch_stream<4, 4, 4>, 0.57f, 1.652f, 2.760f, 0.1325f},
 };
 struct TileKind {
   int bm, bn;
@@ -522,10 +553,10 @@ struct TileKind {
   float call, step, step_full, outputs, join, partial;
 };
 const TileKind kTiles[] = {
-    {64, 128, launch_tiles<1, 1, 2, 4, 4>, 4.03f, 0.38f, 0.01f, 1.39f, 3.28f, 0.25f},
-    {128, 128, launch_tiles<2, 1, 2, 4, 3>, 4.54f, 0.42f, 0.147f, 1.0f, 3.34f, 0.29f},
-    {128, 256, launch_tiles<2, 2, 2, 4, 2>, 5.45f, 0.72f, 0.31f, 1.06f, 3.87f, 0.277f},
-    {256, 256, launch_tiles<4, 2, 2, 4, 2>, 7.15f, 1.10f, 0.325f, 4.77f, 6.25f, 0.197f},
+    {64, 128, launch_tiles<1, 1, 2, 4, 4>, 3.97f, 0.398f, 0.017f, 1.53f, 3.18f, 0.229f},
+    {128, 128, launch_tiles<2, 1, 2, 4, 3>, 4.21f, 0.472f, 0.060f, 1.76f, 3.34f, 0.268f},
+    {128, 256, launch_tiles<2, 2, 2, 4, 2>, 5.07f, 0.769f, 0.142f, 2.76f, 3.60f, 0.263f},
+    {256, 256, launch_tiles<4, 2, 2, 4, 2>, 6.68f, 1.155f, 0.299f, 3.04f, 4.08f, 0.289f},
 };
 
 struct Plan {
@@ -538,11 +569,11 @@ Plan plan_of(int64_t M, int64_t N, int K) {
   const int ktot = K / kTileK, steps = steps_of(K);
   for (int i = 0; i < (int)(sizeof kStream / sizeof kStream[0]); ++i) {
     const StreamKind &k = kStream[i];
-    const int64_t groups = (N / 16 + k.nc - 1) / k.nc * ((M + 16 * k.mt - 1) / (16 * k.mt));
+    const int64_t groups = ((N / 16 + k.nc - 1) / k.nc + 7) / 8 * 8 * ((M + 16 * k.mt - 1) / (16 * k.mt));
     if (groups > 0x7FFFFFFF) continue;
     const float rounds = (float)((groups + kUnits - 1) / kUnits);
-    const int per = (ktot + k.nw - 1) / k.nw, u = k.mt * k.nc >= 4 ? 2 : 4;
-    const float t = k.call + k.batch * (float)((per + u - 1) / u) + rounds * (k.group + (float)ktot * ((float)k.nc * k.column + (float)k.mt * k.row));
+    const int batches = (ktot + 4 * k.nw - 1) / (4 * k.nw);
+    const float t = k.call + k.batch * (float)batches + rounds * k.group + (rounds - 1.0f) * (float)ktot * k.step;
     if (t < least) least = t, best = Plan{i, -1, 1};
   }
   for (int i = 0; i < (int)(sizeof kTiles / sizeof kTiles[0]); ++i) {

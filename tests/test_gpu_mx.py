@@ -123,7 +123,7 @@ def test_product(M, N, K):
 @pytest.mark.parametrize("M,N,K", [(300, 512, 512), (513, 784, 1024), (1000, 272, 4096), (700, 2048, 384), (2049, 1040, 256),
                                    (260, 16384, 128), (816, 16384, 640), (2100, 8208, 384), (1500, 4112, 896), (4100, 4112, 1152),
                                    (300, 256, 16384), (520, 2048, 8320), (816, 2048, 16384), (390, 272, 32768), (260, 1024, 7552),
-                                   (3000, 16384, 2176), (129, 32768, 256)])
+                                   (3000, 16384, 2176), (129, 32768, 256), (1338, 64, 12032), (620, 752, 12928), (1100, 80, 32640)])
 def test_product_of_many_rows(M, N, K):
     flush(f"mx_gemm M={M} N={N} K={K}")
     a, sa = operands(M, K, M)
@@ -141,6 +141,10 @@ def test_product_of_many_rows(M, N, K):
     assert bool((off <= size * 2.0 ** -23 * (K // 32 + 8) + want.abs() * (HALF_BF16 + 2.0 ** -22) + slack).all())
     assert bool((out[M:] == 5).all()) and bool((out[:, N:] == 5).all())
     assert torch.equal(fq().mx_gemm(*args), out[:M, :N])
+
+
+def test_some_of_those_split_k():
+    assert all(fq().mx_gemm_workspace_bytes(M, N, K) > 0 for M, N, K in ((816, 2048, 16384), (1100, 80, 32640)))
 
 
 @pytest.mark.parametrize("M", [1, 40, 300])

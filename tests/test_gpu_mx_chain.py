@@ -108,11 +108,11 @@ def test_another_stream():
     assert f._gpu_stream(0) == torch.cuda.current_stream().cuda_stream
 
 
-@pytest.mark.parametrize("M,N,split", [(390, 272, False), (390, 2048, True)])
-def test_two_streams_at_once_with_workspaces_of_their_own(M, N, split):
+@pytest.mark.parametrize("split", [False, True])
+def test_two_streams_at_once_with_workspaces_of_their_own(split):
     """Products on two streams, many times over, the split ones each with its own partial sums."""
-    f, K = fq(), 16384
-    assert (f.mx_gemm_workspace_bytes(M, N, K) > 0) == split
+    f, K, N = fq(), 32768, 64
+    M = next(m for m in range(37, 2000, 97) if (f.mx_gemm_workspace_bytes(m, N, K) > 0) == split)
     r = np.random.default_rng(0)
     lin = f.MXLinear(dev((r.standard_normal((N, K)) * 0.02).astype(np.float32)), 128)
     xs = [f.mx_quant(dev_bf16(tokens(M, K, s, special=False)), 128) for s in (1, 2)]
