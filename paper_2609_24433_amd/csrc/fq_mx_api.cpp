@@ -285,13 +285,18 @@ fq_status fq_mx_linear(const void *x_bf16, int64_t ldx, const float *smooth_inv,
                      span(w_scales, mx_scales_bytes(N, K)), floats(bias, N)}))
     return fail(FQ_ERR_ALIAS, "y and the workspace must not overlap each other or an input");
   uint8_t *codes = static_cast<uint8_t *>(ws), *scales = codes + align256(mx_codes_bytes(M, K));
-  hipStream_t st = static_cast<hipStream_t>(stream);
-  hipError_t e = launch_mx_quant(quant_args(x_bf16, false, ldx, smooth_inv, post_inv, M, K, b, codes, scales), st);
-  if (e != hipSuccess) return hip_fail(e, "mx quantization launch");
+  const MxQuantArgs q = quant_args(x_bf16, false, ldx, smooth_inv, post_inv, M, K, b, codes, scales);
   const MxGemmArgs g{codes, scales, static_cast<const uint8_t *>(w_packed), static_cast<const uint8_t *>(w_scales), bias,
                      static_cast<uint16_t *>(y_bf16), ldy, M, N, (int)K};
-  e = launch_mx_gemm(g, scales + align256(mx_scales_bytes(M, K)), st);
-  return e == hipSuccess ? ok() : hip_fail(e, "mx product launch");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  if (mx_token_fits(M, N, (int)K)) {
+    e = launch_mx_token(q, g, st);
+  } else {
+    e = launch_mx_quant(q, st);
+    if (e == hipSuccess) e = launch_mx_gemm(g, scales + align256(mx_scales_bytes(M, K)), st);
+  }
+  return e == hipSuccess ? ok() : hip_fail(e, "mx projection launch");
 }
 
 }  // extern "C"

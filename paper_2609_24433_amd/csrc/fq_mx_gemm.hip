@@ -28,6 +28,53 @@ __device__ __forceinline__ v4f mfma_mx_16(const v4i &a, int sa, const v4i &b, in
 #endif
 }
 
+// The bias of the four columns of a lane's sums in join_waves, asked for before the product: behind it the load costs a
+// microsecond and more.
+template <int NC>
+__device__ __forceinline__ float4 bias_of(const MxGemmArgs &p, int64_t n0, int cols) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = 16 * (wave % NC) + 4 * (lane >> 4);
+  return p.bias && n < cols ? *reinterpret_cast<const float4 *>(p.bias + n0 + n) : make_float4(0.f, 0.f, 0.f, 0.f);
+}
+
+// Every wave's sums side by side; each lane's four columns of one row are added up in the order of the waves.
+template <int MT, int NC, int NW>
+__device__ __forceinline__ void join_waves(const v4f (&acc)[MT][NC], uint8_t *lds, const MxGemmArgs &p, float4 bias, int64_t m0, int64_t n0,
+                                           int rows, int cols) {
+  static_assert(NW % NC == 0, "a wave joins tiles of one column block");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+  constexpr int TILES = MT * NC;
+  float4 *sums = reinterpret_cast<float4 *>(lds);
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      sums[(wave * TILES + t * NC + c) * 64 + lane] = make_float4(acc[t][c][0], acc[t][c][1], acc[t][c][2], acc[t][c][3]);
+  __syncthreads();
+  for (int tile = wave; tile < TILES; tile += NW) {
+    float4 v = sums[tile * 64 + lane];
+#pragma unroll
+    for (int s = 1; s < NW; ++s) {
+      const float4 x4 = sums[(s * TILES + tile) * 64 + lane];
+      v.x += x4.x;
+      v.y += x4.y;
+      v.z += x4.z;
+      v.w += x4.w;
+    }
+    const int t = tile / NC, c = tile - t * NC;
+    const int m = 16 * t + r16, n = 16 * c + 4 * g;
+    if (m >= rows || n >= cols) continue;
+    if (p.bias) {
+      v.x += bias.x;
+      v.y += bias.y;
+      v.z += bias.z;
+      v.w += bias.w;
+    }
+    *reinterpret_cast<uint2 *>(p.y + (m0 + m) * p.ldy + n0 + n) =
+        make_uint2(f32_to_bf16(v.x) | (f32_to_bf16(v.y) << 16), f32_to_bf16(v.z) | (f32_to_bf16(v.w) << 16));
+  }
+}
+
 // Few rows: the stream of the weights.  A workgroup has 16 NC columns and 16 MT rows; its NW waves share out K in batches of
 // four steps of 128 channels, ask for every load of a batch before they multiply the one ahead, and their sums meet in LDS.
 //   In product i of a batch lane group g multiplies block i of step g: a lane's four scale bytes are one word, loaded once.
@@ -49,6 +96,7 @@ __global__ __launch_bounds__(64 * NW) void mx_gemm_stream_kernel(MxGemmArgs p) {
   const int k1 = min((wave + 1) * per, ktot);
   int k0 = wave * per;
 
+  const float4 bias = bias_of<NC>(p, n0, cols);
   // A KB of LDS has a step of 16 rows, their four pieces exchanged by (row >> 2) & 3 against bank conflicts.  What lies
   // behind the rows or columns is not stored.
   const uint8_t *a0 = p.a + m0 * (p.K / 2), *w0 = p.w + n0 / 16 * ktot * 1024;
@@ -124,39 +172,107 @@ __global__ __launch_bounds__(64 * NW) void mx_gemm_stream_kernel(MxGemmArgs p) {
   }
   wait_vmcnt<0>();  // the trailing loads are over: LDS is reused
 
-  // every wave's sums side by side; each lane's four columns of one row are added up in the order of the waves
-  constexpr int TILES = MT * NC;
-  float4 *sums = reinterpret_cast<float4 *>(lds);
-  __syncthreads();
+  join_waves<MT, NC, NW>(acc, lds, p, bias, m0, n0, rows, cols);
+}
+
+struct TokenParams {
+  MxQuantArgs q;
+  MxGemmArgs g;
+  int log2b;
+};
+
+// One or two tokens from bf16: the streaming kernel with the rounding inside.  While a batch's weights are on their way, its
+// wave rounds the same channels of the rows (16 lanes a 256-channel piece, as mx_quant's kernel, so the codes are the same)
+// into its part of LDS.  Every workgroup rounds the rows anew, which at this height costs less than a launch: 2048 to 16384
+// 4.0 us in a graph and 6.0 to 6.4 as two launches, 1024 to 4096 3.2 and 4.7, 4096 to 4096 4.4 and 5.4.  (The next batch's
+// rows and weights asked for ahead cost a single batch 0.2 to 0.6 us more and saved eight 0.9.)
+template <int NC, int NW>
+__global__ __launch_bounds__(64 * NW) void mx_token_kernel(TokenParams p) {
+  constexpr int ROOM = 4096 + 256;  // codes and scale words of 16 rows and a batch
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[NW * (ROOM > NC * 1024 ? ROOM : NC * 1024)];
+  const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t n0 = (int64_t)blockIdx.x * 16 * NC;
+  const int rows = (int)p.g.M, cols = min((int)p.g.N - (int)n0, 16 * NC);
+  const int ktot = p.g.K / kTileK, per = ((ktot + 4 * NW - 1) / (4 * NW)) * 4;
+  const int k0 = wave * per, k1 = min(k0 + per, ktot);
+
+  const float4 bias = bias_of<NC>(p.g, n0, cols);
+  const __amdgpu_buffer_rsrc_t wr = buffer_of(p.g.w + n0 / 16 * ktot * 1024, cols / 16 * ktot * 1024);
+  const uint32_t wvoff = g * 1024u + r16 * 16u;
+  const uint32_t *sw[NC];
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
+  for (int c = 0; c < NC; ++c) sw[c] = reinterpret_cast<const uint32_t *>(p.g.w_scale) + n0 + min(16 * c + r16, cols - 1);
+  // lanes 0 to 31 hold the first row's 32 chunks of a batch, the others the second's
+  const int row = lane >> 5, piece = (lane & 16) | mx_chunk(r16);
+  const int64_t at = (int64_t)min(row, rows - 1) * p.q.ldx;
+
+  struct Rows {
+    Chunk<uint16_t> x;
+    float4 pre[4], post[4];
+  };
+  struct Weights {
+    v4i w[NC][4];
+    uint32_t s[NC];
+  };
+  auto load = [&](Rows &a, Weights &b, int k) {
+    const int j = min(k * 8 + piece, ktot * 8 - 1);
+    load_chunk<uint16_t>(p.q.x, at + (int64_t)j * 16, a.x);
+    if (p.q.pre) load_mult(p.q.pre, j, a.pre);
+    if (p.q.post) load_mult(p.q.post, j, a.post);
 #pragma unroll
     for (int c = 0; c < NC; ++c)
-      sums[(wave * TILES + t * NC + c) * 64 + lane] = make_float4(acc[t][c][0], acc[t][c][1], acc[t][c][2], acc[t][c][3]);
-  __syncthreads();
-  for (int tile = wave; tile < TILES; tile += NW) {
-    float4 v = sums[tile * 64 + lane];
 #pragma unroll
-    for (int s = 1; s < NW; ++s) {
-      const float4 x4 = sums[(s * TILES + tile) * 64 + lane];
-      v.x += x4.x;
-      v.y += x4.y;
-      v.z += x4.z;
-      v.w += x4.w;
+      for (int i = 0; i < 4; ++i)
+        b.w[c][i] = __builtin_amdgcn_raw_buffer_load_b128(wr, wvoff + i * 256u + (uint32_t)c * (uint32_t)ktot * 1024u, (uint32_t)k * 1024u, 0);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) b.s[c] = sw[c][(int64_t)min(k + g, ktot - 1) * p.g.N];
+  };
+  uint8_t *mine = lds + wave * ROOM;
+  uint32_t *scales = reinterpret_cast<uint32_t *>(mine + 4096);
+  auto round = [&](const Rows &a) {
+    float v[1][16];
+    unpack_chunk<uint16_t>(a.x, v[0]);
+    if (p.q.pre) mul_chunk(v[0], a.pre);
+    if (p.log2b) {
+      const float f = mx_transform<1>(v, p.log2b, r16) * p.q.cb;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[0][i] *= f;
     }
-    const int t = tile / NC, c = tile - t * NC;
-    const int m = 16 * t + r16, n = 16 * c + 4 * g;
-    if (m >= rows || n >= cols) continue;
-    if (p.bias) {
-      const float4 b = *reinterpret_cast<const float4 *>(p.bias + n0 + n);
-      v.x += b.x;
-      v.y += b.y;
-      v.z += b.z;
-      v.w += b.w;
+    if (p.q.post) mul_chunk(v[0], a.post);
+    const uint32_t byte = mx_scale_byte(block_max(v[0]));
+    const uint2 code = mx_pack16(v[0], byte);
+    const uint32_t word = step_scales(byte, r16);
+    if (row < rows) {
+      *reinterpret_cast<uint2 *>(mine + (piece >> 3) * 1024 + row * 64 + (piece & 7) * 8) = code;
+      if ((r16 & 11) == 0) scales[(piece >> 3) * 16 + row] = word;
     }
-    *reinterpret_cast<uint2 *>(p.y + (m0 + m) * p.ldy + n0 + n) =
-        make_uint2(f32_to_bf16(v.x) | (f32_to_bf16(v.y) << 16), f32_to_bf16(v.z) | (f32_to_bf16(v.w) << 16));
+  };
+  v4f acc[1][NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) acc[0][c] = v4f{0.f, 0.f, 0.f, 0.f};
+  auto multiply = [&](const Weights &b, int k) {
+    const int on = k + g < k1 ? -1 : 0;  // as above
+    const int r = min(r16, rows - 1);    // (the last row again for all behind it, whose outputs are not stored)
+    const uint32_t sa = scales[g * 16 + r];
+    auto product = [&](auto which) {
+      constexpr int i = decltype(which)::value;
+      const v4i a = *reinterpret_cast<const v4i *>(mine + g * 1024 + r * 64 + i * 16);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) acc[0][c] = mfma_mx_16<i>(b.w[c][i], (int)b.s[c] & on, a, (int)sa & on, acc[0][c]);
+    };
+    static_for<4>(product);
+  };
+  Rows a;
+  Weights b;
+  for (int k = k0; k < k1; k += 4) {
+    load(a, b, k);
+    round(a);
+    wave_lds_fence();
+    multiply(b, k);
+    wave_lds_fence();
   }
+  join_waves<1, NC, NW>(acc, lds, p.g, bias, 0, n0, rows, cols);
 }
 
 // 32 x 32 x 64: lane l holds row (or column) l % 32 and block l / 32; its scale is byte SEL of sa (sb).
@@ -499,6 +615,12 @@ hipError_t launch_stream(const MxGemmArgs &g, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int NC, int NW>
+hipError_t launch_token(const TokenParams &p, hipStream_t s) {
+  hipLaunchKernelGGL((mx_token_kernel<NC, NW>), dim3((unsigned)((p.g.N + 16 * NC - 1) / (16 * NC))), dim3(64 * NW), 0, s, p);
+  return hipGetLastError();
+}
+
 template <int TI, int TJ, int WM, int WN, int STAGES, bool SPLIT>
 hipError_t launch_tile(TileParams p, hipStream_t s) {
   using T = TileShape<TI, TJ, WM, WN, STAGES>;
@@ -570,7 +692,7 @@ Plan plan_of(int64_t M, int64_t N, int K) {
   for (int i = 0; i < (int)(sizeof kStream / sizeof kStream[0]); ++i) {
     const StreamKind &k = kStream[i];
     const int64_t groups = ((N / 16 + k.nc - 1) / k.nc + 7) / 8 * 8 * ((M + 16 * k.mt - 1) / (16 * k.mt));
-    if (groups > 0x7FFFFFFF) continue;
+    if (groups * 64 * k.nw > 0xFFFFFFFF) continue;  // threads of a launch
     const float rounds = (float)((groups + kUnits - 1) / kUnits);
     const int batches = (ktot + 4 * k.nw - 1) / (4 * k.nw);
     const float t = k.call + k.batch * (float)batches + rounds * k.group + (rounds - 1.0f) * (float)ktot * k.step;
@@ -601,6 +723,25 @@ size_t mx_gemm_workspace(int64_t M, int64_t N, int64_t K) {
 hipError_t launch_mx_gemm(const MxGemmArgs &g, void *ws, hipStream_t s) {
   const Plan p = plan_of(g.M, g.N, g.K);
   return p.tile < 0 ? kStream[p.stream].launch(g, s) : kTiles[p.tile].launch(g, p.splits, static_cast<float *>(ws), s);
+}
+
+// One launch or two: the one rounds each batch of a wave before the product takes it, 1.2 us a batch, and pays up to three or
+// four batches a wave (two waves: 2688 channels 4.9 us and 5.6, 4480 9.0 and 7.2; four waves: 8192 to 1024 outputs 6.1 and 6.1,
+// to 8192 outputs 8.4 and 10.2, 16384 to 2048 11.2 and 8.0).
+bool mx_token_fits(int64_t M, int64_t N, int K) {
+  const Plan p = plan_of(M, N, K);
+  if (M > 2 || p.tile >= 0 || kStream[p.stream].nw > 4) return false;
+  return K <= (kStream[p.stream].nw == 2 ? 3 : 4) * 512 * kStream[p.stream].nw;
+}
+
+// As many waves as the product's own kernel, whose sums these are then to the last bit; columns of a workgroup so that its
+// waves all find room at once (2048 to 32768 outputs: 16 columns 8.8 us, 32 7.2, 64 5.5; 4096 to 4096: 4.3, 4.7 and 5.2).
+hipError_t launch_mx_token(const MxQuantArgs &q, const MxGemmArgs &g, hipStream_t s) {
+  const TokenParams p{q, g, log2_of(q.b)};
+  const int nw = kStream[plan_of(g.M, g.N, g.K).stream].nw;
+  const int64_t waves = g.N / 16 * nw;
+  if (nw == 2) return waves <= 8 * kUnits ? launch_token<1, 2>(p, s) : launch_token<2, 2>(p, s);
+  return waves <= 8 * kUnits ? launch_token<1, 4>(p, s) : waves <= 16 * kUnits ? launch_token<2, 4>(p, s) : launch_token<4, 4>(p, s);
 }
 
 }  // namespace fq

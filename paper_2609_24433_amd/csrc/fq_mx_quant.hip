@@ -19,52 +19,6 @@ namespace fq {
 
 namespace {
 
-// Chunk of lane tau of a 16-lane group: bits 2 and 3 swapped, so that the stage h = 64 is a DPP
-// rotation by 8 lanes and only h = 128 needs the LDS crossbar (as the prologue's kernel).
-__device__ __forceinline__ int mx_chunk(int tau) { return (tau & ~12) | ((tau & 4) << 1) | ((tau & 8) >> 1); }
-
-// The unnormalized block Hadamard of 2^log2b channels (uniform), lanes holding chunks mx_chunk(tau).
-// The values come out times the sign that it returns.
-template <int CPT>
-__device__ __forceinline__ float mx_transform(float (&v)[CPT][16], int log2b, int tau) {
-#pragma unroll
-  for (int c = 0; c < CPT; ++c) {
-    if (log2b > 0) chunk_stage<1>(v[c]);
-    if (log2b > 1) chunk_stage<2>(v[c]);
-    if (log2b > 2) chunk_stage<4>(v[c]);
-    if (log2b > 3) chunk_stage<8>(v[c]);
-  }
-  int mask = 0;
-  if (log2b > 4) lane_stage<1, CPT>(v, tau), mask |= 1;
-  if (log2b > 5) lane_stage<2, CPT>(v, tau), mask |= 2;
-  if (log2b > 6) lane_stage<8, CPT>(v, tau), mask |= 8;
-  if (log2b > 7) lane_stage<4, CPT>(v, tau), mask |= 4;
-  return (__builtin_popcount(tau & mask) & 1) ? -1.0f : 1.0f;
-}
-
-__device__ __forceinline__ void load_mult(const float *m, int chunk, float4 (&f)[4]) {
-  const float4 *p = reinterpret_cast<const float4 *>(m) + (int64_t)chunk * 4;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) f[i] = p[i];
-}
-
-// max |v| of a block's 32 channels: the chunk's 16 and those of the lane next to it.
-__device__ __forceinline__ float block_max(const float (&v)[16]) {
-  float m = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 16; i += 2) m = abs_maximum(m, v[i], v[i + 1]);
-  return maximum(m, lane_xor<1>(m));
-}
-
-// The four scale bytes of a 128-channel step, in all of its eight lanes (chunk bits 1, 2 are lane bits
-// 1, 3).
-__device__ __forceinline__ uint32_t step_scales(uint32_t byte, int tau) {
-  uint32_t w = byte << (8 * (((tau >> 1) & 1) | ((tau >> 2) & 2)));
-  w |= __float_as_uint(lane_xor<2>(__uint_as_float(w)));
-  w |= __float_as_uint(lane_xor<8>(__uint_as_float(w)));
-  return w;
-}
-
 struct MxQuantParams {
   const void *x;
   int64_t ldx;
@@ -361,12 +315,6 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const uint4 *from, int64_t
     if (unpack) to[flat] = from[i];
     else to[i] = from[flat];
   }
-}
-
-int log2_of(int b) {
-  int k = 0;
-  while ((1 << k) < b) ++k;
-  return k;
 }
 
 // The launches of a kernel over 16-channel chunks of rows: chunk numbers of one launch fit 32 bits.

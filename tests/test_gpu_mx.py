@@ -189,6 +189,26 @@ def test_projection_is_its_two_halves(M, K, N, b, folds):
     assert_product(y, a, f.mx_read(wc, ws).double().cpu().numpy(), None if bias is None else bias.cpu().numpy())
 
 
+@pytest.mark.parametrize("M,K,N,b", [(1, 128, 16, 128), (2, 384, 80, 128), (2, 640, 2064, 64), (1, 1280, 16384, 256), (2, 1792, 16, 256),
+                                     (1, 2048, 32768, 128), (2, 2432, 5008, 1), (1, 4096, 4096, 32), (2, 2048, 16400, 2), (2, 7680, 48, 16)])
+@pytest.mark.parametrize("folds", [False, True])
+def test_tokens_one_by_one_or_many(M, K, N, b, folds):
+    """A token's outputs do not depend on how the rounding and the product are launched, nor on its neighbour."""
+    flush(f"mx_linear M={M} K={K} N={N} b={b}")
+    f, r = fq(), np.random.default_rng(K + N)
+    x = strided(tokens(M, K, 3, special=False))
+    pre, post = (dev(r.uniform(0.5, 2, K).astype(np.float32)) for _ in range(2)) if folds else (None, None)
+    w, sw = operands(N, K, 7)
+    packed, sw = f.mx_pack(dev(mx.pack_nibbles(w))), dev(mx.steps(sw))
+    bias = dev(r.standard_normal(N).astype(np.float32)) if folds else None
+    y = f.mx_linear(x, packed, sw, b, pre, post, bias)
+    assert torch.equal(y, f.mx_gemm(*f.mx_quant(x, b, pre, post), packed, sw, bias))
+    bad = x.clone()
+    bad[M - 1, K // 3] = float("inf")
+    y_bad = f.mx_linear(bad, packed, sw, b, pre, post, bias)
+    assert torch.equal(y_bad[:M - 1], y[:M - 1]) and torch.isnan(y_bad[M - 1]).all()
+
+
 def test_no_rows():
     f = fq()
     x = torch.zeros((0, 256), dtype=torch.bfloat16, device=DEV)
