@@ -65,11 +65,18 @@ struct MxGemmArgs {
   int64_t M, N;
   int K;
 };
-size_t mx_gemm_workspace(int64_t M, int64_t N, int64_t K);
-hipError_t launch_mx_gemm(const MxGemmArgs &g, void *ws, hipStream_t s);
-// Rounding and product in one launch, where that is faster than two; the same outputs.  g.a and g.a_scale are not used.
-bool mx_token_fits(int64_t M, int64_t N, int K);
-hipError_t launch_mx_token(const MxQuantArgs &q, const MxGemmArgs &g, hipStream_t s);
+// How a product of these sizes is launched (mx_plan).
+struct MxPlan {
+  int stream, tile, splits;  // one of stream and tile is -1
+  bool token;                // the projection in one launch
+};
+MxPlan mx_plan(int64_t M, int64_t N, int64_t K);
+inline size_t mx_gemm_workspace(const MxPlan &p, int64_t M, int64_t N) {
+  return p.splits > 1 ? (size_t)p.splits * (size_t)M * (size_t)N * 4 : 0;
+}
+hipError_t launch_mx_gemm(const MxGemmArgs &g, const MxPlan &p, void *ws, hipStream_t s);
+// Rounding and product in one launch (p.token), the same outputs.  g.a, g.a_scale and q's outputs are not used.
+hipError_t launch_mx_token(const MxQuantArgs &q, const MxGemmArgs &g, const MxPlan &p, hipStream_t s);
 
 #if defined(__HIPCC__)
 

@@ -179,6 +179,14 @@ fq_status read_common(const void *codes, const void *scale, int64_t M, int64_t K
   return e == hipSuccess ? ok() : hip_fail(e, "read launch");
 }
 
+bool product_sizes(int64_t M, int64_t N, int64_t K) {
+  return M > 0 && N > 0 && M <= kMaxRows && N <= kMaxRows && K >= 128 && K <= kMaxK;
+}
+
+size_t linear_workspace(const MxPlan &p, int64_t M, int64_t N, int64_t K) {
+  return p.token ? 0 : align256(mx_codes_bytes(M, K)) + align256(mx_scales_bytes(M, K)) + mx_gemm_workspace(p, M, N);
+}
+
 fq_status check_room(const void *ws, size_t have, size_t need) {
   if (need > 0 && (!ws || have < need))
     return fail(FQ_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, ws ? have : (size_t)0);
@@ -242,7 +250,7 @@ fq_status fq_mx_unpack(const void *packed, int64_t N, int64_t K, void *codes, vo
 }
 
 size_t fq_mx_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-  return M <= 0 || N <= 0 || K < 128 ? 0 : mx_gemm_workspace(M, N, K);
+  return !product_sizes(M, N, K) ? 0 : mx_gemm_workspace(mx_plan(M, N, K), M, N);
 }
 
 fq_status fq_mx_gemm(const void *a_codes, const void *a_scales, const void *w_packed, const void *w_scales, const float *bias,
@@ -252,7 +260,8 @@ fq_status fq_mx_gemm(const void *a_codes, const void *a_scales, const void *w_pa
   if (!a_codes || !a_scales || !w_packed || !w_scales || !y_bf16)
     return fail(FQ_ERR_NULL, "a_codes, a_scales, w_packed, w_scales and y must be non-NULL");
   FQ_TRY(check_aligned({a_codes, a_scales, w_packed, w_scales, bias, y_bf16}));
-  const size_t need = mx_gemm_workspace(M, N, K);
+  const MxPlan plan = mx_plan(M, N, K);
+  const size_t need = mx_gemm_workspace(plan, M, N);
   FQ_TRY(check_room(ws, ws_bytes, need));
   if (outputs_alias({rows_of(y_bf16, M, ldy, N, 2), span(need ? ws : nullptr, need)},
                     {span(a_codes, mx_codes_bytes(M, K)), span(a_scales, mx_scales_bytes(M, K)), span(w_packed, mx_codes_bytes(N, K)),
@@ -261,13 +270,12 @@ fq_status fq_mx_gemm(const void *a_codes, const void *a_scales, const void *w_pa
   const MxGemmArgs g{static_cast<const uint8_t *>(a_codes), static_cast<const uint8_t *>(a_scales),
                      static_cast<const uint8_t *>(w_packed), static_cast<const uint8_t *>(w_scales), bias,
                      static_cast<uint16_t *>(y_bf16), ldy, M, N, (int)K};
-  const hipError_t e = launch_mx_gemm(g, ws, static_cast<hipStream_t>(stream));
+  const hipError_t e = launch_mx_gemm(g, plan, ws, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ok() : hip_fail(e, "mx product launch");
 }
 
 size_t fq_mx_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-  if (M <= 0 || N <= 0 || K < 128) return 0;
-  return align256(mx_codes_bytes(M, K)) + align256(mx_scales_bytes(M, K)) + mx_gemm_workspace(M, N, K);
+  return !product_sizes(M, N, K) ? 0 : linear_workspace(mx_plan(M, N, K), M, N, K);
 }
 
 fq_status fq_mx_linear(const void *x_bf16, int64_t ldx, const float *smooth_inv, const float *post_inv, int64_t M, int64_t K,
@@ -278,23 +286,25 @@ fq_status fq_mx_linear(const void *x_bf16, int64_t ldx, const float *smooth_inv,
   if (M == 0 || N == 0) return ok();
   if (!x_bf16 || !w_packed || !w_scales || !y_bf16) return fail(FQ_ERR_NULL, "x, w_packed, w_scales and y must be non-NULL");
   FQ_TRY(check_aligned({x_bf16, w_packed, w_scales, bias, y_bf16}));
-  const size_t need = fq_mx_linear_workspace_bytes(M, N, K);
+  const MxPlan plan = mx_plan(M, N, K);
+  const size_t need = linear_workspace(plan, M, N, K);
   FQ_TRY(check_room(ws, ws_bytes, need));
-  if (outputs_alias({rows_of(y_bf16, M, ldy, N, 2), span(ws, need)},
+  if (outputs_alias({rows_of(y_bf16, M, ldy, N, 2), span(need ? ws : nullptr, need)},
                     {rows_of(x_bf16, M, ldx, K, 2), floats(smooth_inv, K), floats(post_inv, K), span(w_packed, mx_codes_bytes(N, K)),
                      span(w_scales, mx_scales_bytes(N, K)), floats(bias, N)}))
     return fail(FQ_ERR_ALIAS, "y and the workspace must not overlap each other or an input");
-  uint8_t *codes = static_cast<uint8_t *>(ws), *scales = codes + align256(mx_codes_bytes(M, K));
+  // codes and scales of the workspace; a launch that rounds for itself has none
+  uint8_t *codes = static_cast<uint8_t *>(ws), *scales = plan.token ? nullptr : codes + align256(mx_codes_bytes(M, K));
   const MxQuantArgs q = quant_args(x_bf16, false, ldx, smooth_inv, post_inv, M, K, b, codes, scales);
   const MxGemmArgs g{codes, scales, static_cast<const uint8_t *>(w_packed), static_cast<const uint8_t *>(w_scales), bias,
                      static_cast<uint16_t *>(y_bf16), ldy, M, N, (int)K};
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e;
-  if (mx_token_fits(M, N, (int)K)) {
-    e = launch_mx_token(q, g, st);
+  if (plan.token) {
+    e = launch_mx_token(q, g, plan, st);
   } else {
     e = launch_mx_quant(q, st);
-    if (e == hipSuccess) e = launch_mx_gemm(g, scales + align256(mx_scales_bytes(M, K)), st);
+    if (e == hipSuccess) e = launch_mx_gemm(g, plan, scales + align256(mx_scales_bytes(M, K)), st);
   }
   return e == hipSuccess ? ok() : hip_fail(e, "mx projection launch");
 }

@@ -681,14 +681,20 @@ const TileKind kTiles[] = {
     {256, 256, launch_tiles<4, 2, 2, 4, 2>, 6.68f, 1.155f, 0.299f, 3.04f, 4.08f, 0.289f},
 };
 
-struct Plan {
-  int stream, tile, splits;  // one of stream and tile is -1
-};
+// One launch or two: the one rounds each batch of a wave before the product takes it, 1.2 us a batch, and pays up to three or
+// four batches a wave (two waves: 2688 channels 4.9 us and 5.6, 4480 9.0 and 7.2; four waves: 8192 to 1024 outputs 6.1 and 6.1,
+// to 8192 outputs 8.4 and 10.2, 16384 to 2048 11.2 and 8.0).
+bool one_launch(const MxPlan &p, int64_t M, int K) {
+  if (M > 2 || p.tile >= 0 || kStream[p.stream].nw > 4) return false;
+  return K <= (kStream[p.stream].nw == 2 ? 3 : 4) * 512 * kStream[p.stream].nw;
+}
 
-Plan plan_of(int64_t M, int64_t N, int K) {
-  Plan best{0, -1, 1};
+}  // namespace
+
+MxPlan mx_plan(int64_t M, int64_t N, int64_t K) {
+  MxPlan best{0, -1, 1, false};
   float least = INFINITY;
-  const int ktot = K / kTileK, steps = steps_of(K);
+  const int ktot = (int)K / kTileK, steps = steps_of((int)K);
   for (int i = 0; i < (int)(sizeof kStream / sizeof kStream[0]); ++i) {
     const StreamKind &k = kStream[i];
     const int64_t groups = ((N / 16 + k.nc - 1) / k.nc + 7) / 8 * 8 * ((M + 16 * k.mt - 1) / (16 * k.mt));
@@ -696,7 +702,7 @@ Plan plan_of(int64_t M, int64_t N, int K) {
     const float rounds = (float)((groups + kUnits - 1) / kUnits);
     const int batches = (ktot + 4 * k.nw - 1) / (4 * k.nw);
     const float t = k.call + k.batch * (float)batches + rounds * k.group + (rounds - 1.0f) * (float)ktot * k.step;
-    if (t < least) least = t, best = Plan{i, -1, 1};
+    if (t < least) least = t, best = MxPlan{i, -1, 1, false};
   }
   for (int i = 0; i < (int)(sizeof kTiles / sizeof kTiles[0]); ++i) {
     const TileKind &k = kTiles[i];
@@ -707,38 +713,22 @@ Plan plan_of(int64_t M, int64_t N, int K) {
       const float rounds = (float)((pieces + kUnits - 1) / kUnits), full = (float)pieces / (rounds * (float)kUnits);
       float t = k.call + rounds * ((float)per * (k.step + k.step_full * full) + k.outputs * full);
       if (splits > 1) t += k.join + k.partial * (float)splits * (float)M * (float)N * 4e-6f;
-      if (t < least) least = t, best = Plan{-1, i, splits};
+      if (t < least) least = t, best = MxPlan{-1, i, splits, false};
     }
   }
+  best.token = one_launch(best, M, (int)K);
   return best;
 }
 
-}  // namespace
-
-size_t mx_gemm_workspace(int64_t M, int64_t N, int64_t K) {
-  const Plan p = plan_of(M, N, (int)K);
-  return p.splits > 1 ? (size_t)p.splits * (size_t)M * (size_t)N * 4 : 0;
-}
-
-hipError_t launch_mx_gemm(const MxGemmArgs &g, void *ws, hipStream_t s) {
-  const Plan p = plan_of(g.M, g.N, g.K);
+hipError_t launch_mx_gemm(const MxGemmArgs &g, const MxPlan &p, void *ws, hipStream_t s) {
   return p.tile < 0 ? kStream[p.stream].launch(g, s) : kTiles[p.tile].launch(g, p.splits, static_cast<float *>(ws), s);
-}
-
-// One launch or two: the one rounds each batch of a wave before the product takes it, 1.2 us a batch, and pays up to three or
-// four batches a wave (two waves: 2688 channels 4.9 us and 5.6, 4480 9.0 and 7.2; four waves: 8192 to 1024 outputs 6.1 and 6.1,
-// to 8192 outputs 8.4 and 10.2, 16384 to 2048 11.2 and 8.0).
-bool mx_token_fits(int64_t M, int64_t N, int K) {
-  const Plan p = plan_of(M, N, K);
-  if (M > 2 || p.tile >= 0 || kStream[p.stream].nw > 4) return false;
-  return K <= (kStream[p.stream].nw == 2 ? 3 : 4) * 512 * kStream[p.stream].nw;
 }
 
 // As many waves as the product's own kernel, whose sums these are then to the last bit; columns of a workgroup so that its
 // waves all find room at once (2048 to 32768 outputs: 16 columns 8.8 us, 32 7.2, 64 5.5; 4096 to 4096: 4.3, 4.7 and 5.2).
-hipError_t launch_mx_token(const MxQuantArgs &q, const MxGemmArgs &g, hipStream_t s) {
+hipError_t launch_mx_token(const MxQuantArgs &q, const MxGemmArgs &g, const MxPlan &plan, hipStream_t s) {
   const TokenParams p{q, g, log2_of(q.b)};
-  const int nw = kStream[plan_of(g.M, g.N, g.K).stream].nw;
+  const int nw = kStream[plan.stream].nw;
   const int64_t waves = g.N / 16 * nw;
   if (nw == 2) return waves <= 8 * kUnits ? launch_token<1, 2>(p, s) : launch_token<2, 2>(p, s);
   return waves <= 8 * kUnits ? launch_token<1, 4>(p, s) : waves <= 16 * kUnits ? launch_token<2, 4>(p, s) : launch_token<4, 4>(p, s);

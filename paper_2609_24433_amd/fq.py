@@ -7,6 +7,7 @@ If libfq.so is missing the import fails loudly; there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 import struct
@@ -931,6 +932,7 @@ def _mx_operands(w: torch.Tensor, scales: torch.Tensor, bias, out, like, M: int,
     return (N, at, s, b, out, *_matrix(out, _BF16, (M, N), "out", dev))
 
 
+@functools.lru_cache(4096)  # a call asks every time
 def mx_gemm_workspace_bytes(M: int, N: int, K: int) -> int:
     return int(LIB.fq_mx_gemm_workspace_bytes(M, N, K))
 
@@ -943,7 +945,7 @@ def mx_gemm(a_codes: torch.Tensor, a_scales: torch.Tensor, w_packed: torch.Tenso
     N, w, sw, b, out, y, ldy = _mx_operands(w_packed, w_scales, bias, out, a_codes, M, K, dev)
     stream = _gpu_stream(dev)
     if ws is None:
-        ws = _scratch(LIB.fq_mx_gemm_workspace_bytes(M, N, K), a_codes.device)
+        ws = _scratch(mx_gemm_workspace_bytes(M, N, K), a_codes.device)
     room, size = _room(ws, dev)
     rc = LIB.fq_mx_gemm(a, sa, w, sw, b, y, ldy, M, N, K, room, size, stream)
     if rc:
@@ -951,6 +953,7 @@ def mx_gemm(a_codes: torch.Tensor, a_scales: torch.Tensor, w_packed: torch.Tenso
     return out
 
 
+@functools.lru_cache(4096)  # a call asks every time
 def mx_linear_workspace_bytes(M: int, N: int, K: int) -> int:
     return int(LIB.fq_mx_linear_workspace_bytes(M, N, K))
 
@@ -968,7 +971,7 @@ def mx_linear(x: torch.Tensor, w_packed: torch.Tensor, w_scales: torch.Tensor, b
     N, w, sw, bias_at, out, y, ldy = _mx_operands(w_packed, w_scales, bias, out, x, M, K, dev)
     stream = _gpu_stream(dev)
     if ws is None:
-        ws = _scratch(LIB.fq_mx_linear_workspace_bytes(M, N, K), x.device)
+        ws = _scratch(mx_linear_workspace_bytes(M, N, K), x.device)
     room, size = _room(ws, dev)
     rc = LIB.fq_mx_linear(at, ld, pre, post, M, K, N, b, w, sw, bias_at, y, ldy, room, size, stream)
     if rc:
