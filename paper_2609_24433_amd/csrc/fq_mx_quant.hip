@@ -4,13 +4,21 @@
 // product one rounding), then per block of 32 channels the scale 2^e, e = floor(log2 max |u|) - 2, and
 // the nearest E2M1 value of u 2^-e.  No reduction is wider than a block, so rows are not looked
 // at: threads take 16-channel chunks of all rows in a row, and a b-block is b / 16 lanes of a
-// 16-lane group, as in the prologue.
+// 16-lane group, as in the prologue.  Bound by memory: 4095 x 16384 bf16 (170 MB) 32 us, 5.3 TB/s, what a large
+// copy reaches; 38 us with one fold and 43 with both, which every row reads again from the L2, 4 bytes a channel to its own 2.5
+// (two rows a thread share them: 37 and 39 us, but 5 to 10% more for every call under 30 us, and four rows are slower
+// still).  16384 x 2048 fp32 26 us, 5.9 TB/s.  50 x 1024 takes 3.4 us, a launch and one way to memory and back.
 //
 // norm: h = bf16(x + r); s = 1 / sqrt(mean h^2 + eps) with the sum and the root in fp64 (a bf16's
 // square is exact there and the sum all but exact, so s does not depend on the order and the codes can
 // be reproduced bit for bit; in fp32 every order gives other last bits, and other codes next to a
 // tie); y = (h s) w; then the prologue's transform and rounding, or mx_quant's.  A row stays in
-// registers between its two reductions.
+// registers between its two reductions, so it is read once.  Bound by memory: 16383 x 4096 to 8 bits with a residual (470 MB)
+// 92 us, 5.1 TB/s; 816 x 2048 5.4 us.  One row of 2048 takes 4.2 us: the rows' way from memory, the sum over lanes and
+// waves (lane moves instead of the LDS crossbar, 4.5 us -> 4.2), fp64 division and root, the gain's way, the largest value.
+//
+// read: code times scale, one rounding to bf16 (microscaled values need none).  16383 x 4096 8-bit codes (201 MB) 35 us, 5.7
+// TB/s.
 #include "fq_codes.hpp"
 #include "fq_launch.hpp"
 #include "fq_mx.hpp"
@@ -82,8 +90,13 @@ struct NormParams {
   float qf;
 };
 
-__device__ __forceinline__ double lane_xor_f64(double v, int m) {
-  return __shfl_xor(v, m, kWave);
+// The other lane's double, halves through the lane moves of 32 bits.
+template <int M>
+__device__ __forceinline__ double lane_xor_f64(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __float_as_uint(lane_xor<M>(__uint_as_float((uint32_t)u)));
+  const uint32_t hi = __float_as_uint(lane_xor<M>(__uint_as_float((uint32_t)(u >> 32))));
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
 // A row is held by TPR = 2^tpr_log2 >= 16 consecutive threads, thread tau owning CPT chunks
@@ -116,6 +129,16 @@ __global__ __launch_bounds__(NT) void norm_quant_kernel(NormParams p) {
     }
   }
 
+  // the gain asked for before the sum where few rows hide its way (16384 channels, 816 rows 23.5 -> 22.3 us); with a chunk
+  // a thread its registers cost more (816 rows of 2048 6.0 us, else 5.4)
+  constexpr bool EARLY = CPT > 1;
+  float4 gain[CPT][4];
+  auto load_gain = [&] {
+#pragma unroll
+    for (int c = 0; c < CPT; ++c) load_mult(p.a.weight, c * TPR + lam < nchunks ? c * TPR + lam : 0, gain[c]);
+  };
+  if (EARLY) load_gain();
+
   float v[CPT][16];
   double sum = 0.0;
 #pragma unroll
@@ -143,7 +166,12 @@ __global__ __launch_bounds__(NT) void norm_quant_kernel(NormParams p) {
   }
   // the row's sum: its lanes, then its waves
   const int lim = TPR < kWave ? TPR : kWave;
-  for (int m = 1; m < lim; m *= 2) sum += lane_xor_f64(sum, m);
+  sum += lane_xor_f64<1>(sum);
+  sum += lane_xor_f64<2>(sum);
+  sum += lane_xor_f64<4>(sum);
+  sum += lane_xor_f64<8>(sum);
+  if (lim > 16) sum += lane_xor_f64<16>(sum);
+  if (lim > 32) sum += __shfl_xor(sum, 32, kWave);
   if (TPR > kWave) {
     if ((tid & (kWave - 1)) == 0) red_sum[tid / kWave] = sum;
     __syncthreads();
@@ -152,14 +180,12 @@ __global__ __launch_bounds__(NT) void norm_quant_kernel(NormParams p) {
   }
   const float scale = (float)(1.0 / __builtin_sqrt(sum / (double)p.a.K + (double)p.a.eps));
 
+  if (!EARLY) load_gain();
 #pragma unroll
   for (int c = 0; c < CPT; ++c) {
-    const int j = c * TPR + lam, jc = j < nchunks ? j : 0;
-    float4 m[4];
-    load_mult(p.a.weight, jc, m);
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[c][i] *= scale;
-    mul_chunk(v[c], m);
+    mul_chunk(v[c], gain[c]);
   }
   const float sgn = mx_transform<CPT>(v, p.log2b, t16);
   if constexpr (OUT == kOutMx) {
