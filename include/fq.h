@@ -443,7 +443,8 @@ fq_status fq_mx_unpack(const void *packed, int64_t N, int64_t K, void *codes, vo
 
 /* y bf16 [M, ldy] = bf16_rne(sum over blocks of 2^(ea + ew - 254) sum a w, plus bias[n]): fp32 sums on the
  * matrix cores, in an order that the shape fixes (the same call gives the same bits), so within
- * 2^-23 (K/32 + 8) sum |a w| of the exact sum.  bias: fp32 [N] or NULL.
+ * 2^-23 (K/32 + 8) sum |a w| of the exact sum where the sums stay in fp32's normal range (above it they are infinite or
+ * NaN, below 2^-126 they may come out as zeros).  bias: fp32 [N] or NULL.
  *   ws  scratch of fq_mx_gemm_workspace_bytes bytes (fp32 partial sums of a split K; 0 and NULL allowed
  *       where K is not split), no initialization.  Calls that share one race unless they are ordered. */
 size_t fq_mx_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
@@ -451,7 +452,8 @@ fq_status fq_mx_gemm(const void *a_codes, const void *a_scales, const void *w_pa
                      void *y_bf16, int64_t ldy, int64_t M, int64_t N, int64_t K, void *ws, size_t ws_bytes, void *stream);
 
 /* fq_mx_quant of bf16 tokens, then fq_mx_gemm, the same output bit for bit; codes, scales and partial
- * sums live in ws (fq_mx_linear_workspace_bytes bytes). */
+ * sums live in ws (fq_mx_linear_workspace_bytes bytes; 0, and NULL allowed, where one launch does both: one
+ * or two tokens and K that is not long). */
 size_t fq_mx_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
 fq_status fq_mx_linear(const void *x_bf16, int64_t ldx, const float *smooth_inv, const float *post_inv, int64_t M, int64_t K,
                        int64_t N, int b, const void *w_packed, const void *w_scales, const float *bias, void *y_bf16, int64_t ldy,

@@ -81,6 +81,9 @@ __device__ __forceinline__ void join_waves(const v4f (&acc)[MT][NC], uint8_t *ld
 //   Rows go through the wave's own part of LDS: loaded in operand order (a lane a row) they come at 37 bytes a ns and compute
 //   unit, four lanes a row at 120.  Weights are packed in operand order.
 //   Weights are the left operand, so that a lane comes to hold four adjacent columns of one row.
+// Bound by the way of the weights and by the launch: one token 2048 to 16384 (18 MB) 3.6 us in a graph of calls, 5.0 TB/s; 16384
+// to 2048 5.4; 50 rows of the same 6.1 (11.8 with rows loaded in operand order and a scale word a step); 48 rows 4096 to 4096 4.4.
+// Batches of four steps keep 4 KB a column block in flight a wave; a ring of three did not fit the registers of 4 waves a SIMD.
 template <int MT, int NC, int NW>
 __global__ __launch_bounds__(64 * NW) void mx_gemm_stream_kernel(MxGemmArgs p) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
@@ -318,8 +321,14 @@ struct Piece {
   int rows, cols, first, last, split;
 };
 
-// Workgroups take pieces blockIdx, blockIdx + gridDim, .. and read them as one stream of steps through a ring in LDS:
+// Many rows.  Workgroups take pieces blockIdx, blockIdx + gridDim, .. and read them as one stream of steps through a ring in LDS:
 // the next piece's first steps arrive while the last ones of this are multiplied and its outputs stored.
+// 8191 x 4096 to 16384 with 256 x 256 tiles: 263 to 290 us, 3.8 to 4.2 PFLOP/s.  The matrix cores are busy 55% of the
+// time, at 1.8 GHz: under random codes the card lowers its clock (the instructions alone reach 5.9 PFLOP/s with them, 8.3
+// with zeros).  A step's reads of LDS take as long as its products, and a tile's outputs, staged and stored, 5 us of 34 in
+// which nothing is multiplied.  Measured and slower: weights straight to registers (308 us), steps of 128 channels, one
+// or two workgroups a unit (321), outputs stored in pieces of 64 bytes from exchanged operands (313), four waves with tiles of
+// 128 x 128, and accumulators in ordinary registers (17%).
 template <int TI, int TJ, int WM, int WN, int STAGES, bool SPLIT>
 __global__ __launch_bounds__(64 * WM * WN) void mx_gemm_tile_kernel(TileParams p) {
   using T = TileShape<TI, TJ, WM, WN, STAGES>;

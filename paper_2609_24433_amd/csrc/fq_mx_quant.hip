@@ -86,6 +86,7 @@ __global__ __launch_bounds__(kQuantThreads) void mx_quant_kernel(MxQuantParams p
 
 struct NormParams {
   NormArgs a;
+  int64_t row0;  // first row of this launch
   int log2b, tpr_log2;
   float qf;
 };
@@ -111,7 +112,7 @@ __global__ __launch_bounds__(NT) void norm_quant_kernel(NormParams p) {
   const int row_local = tid >> p.tpr_log2;
   const int tau = tid & (TPR - 1), t16 = tid & 15;
   const int lam = (tau & ~15) | mx_chunk(t16);
-  const int64_t row = (int64_t)blockIdx.x * (NT >> p.tpr_log2) + row_local;
+  const int64_t row = p.row0 + (int64_t)blockIdx.x * (NT >> p.tpr_log2) + row_local;
   const bool row_ok = row < p.a.M;
   const int nchunks = p.a.K >> 4;
   const int w0 = (row_local << p.tpr_log2) / kWave, nw = TPR / kWave;
@@ -391,7 +392,6 @@ hipError_t launch_mx_quant(const MxQuantArgs &a, hipStream_t s) {
 }
 
 hipError_t launch_norm_quant(const NormArgs &a, hipStream_t s) {
-  if (a.M <= 0) return hipSuccess;
   // threads a row and chunks a thread, as the prologue's kernel
   int tpr = 16, cpt = 1, log2 = 0;
   while (tpr < a.K / 16) tpr *= 2;
@@ -401,12 +401,15 @@ hipError_t launch_norm_quant(const NormArgs &a, hipStream_t s) {
   }
   const int nt = tpr > 256 ? tpr : 256;
   while ((1 << log2) < tpr) ++log2;
-  NormParams p{a, log2_of(a.b), log2, a.out_fmt == kOutInt8 ? 127.0f : 7.0f};
-  const int64_t grid = (a.M + nt / tpr - 1) / (nt / tpr);
-  if (nt == 256 && cpt == 1) return launch_norm_shape<1, 256>(p, grid, s);
-  if (nt == 256) return launch_norm_shape<2, 256>(p, grid, s);
-  if (nt == 512) return launch_norm_shape<2, 512>(p, grid, s);
-  return launch_norm_shape<2, 1024>(p, grid, s);
+  NormParams p{a, 0, log2_of(a.b), log2, a.out_fmt == kOutInt8 ? 127.0f : 7.0f};
+  const int64_t most = (1ll << 31) / nt * (nt / tpr);  // rows of a launch, whose threads fit 32 bits
+  for (; p.row0 < a.M; p.row0 += most) {
+    const int64_t rows = a.M - p.row0 < most ? a.M - p.row0 : most, grid = (rows + nt / tpr - 1) / (nt / tpr);
+    const hipError_t e = nt == 256 ? cpt == 1 ? launch_norm_shape<1, 256>(p, grid, s) : launch_norm_shape<2, 256>(p, grid, s)
+                         : nt == 512 ? launch_norm_shape<2, 512>(p, grid, s) : launch_norm_shape<2, 1024>(p, grid, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_read_codes(const uint8_t *codes, const void *scale, int64_t M, int K, int bits, uint16_t *values,
