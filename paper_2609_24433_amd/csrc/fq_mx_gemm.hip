@@ -83,7 +83,6 @@ __device__ __forceinline__ void join_waves(const v4f (&acc)[MT][NC], uint8_t *ld
 //   Weights are the left operand, so that a lane comes to hold four adjacent columns of one row.
 // Bound by the way of the weights and by the launch: one token 2048 to 16384 (18 MB) 3.6 us in a graph of calls, 5.0 TB/s; 16384
 // to 2048 5.4; 50 rows of the same 6.1 (11.8 with rows loaded in operand order and a scale word a step); 48 rows 4096 to 4096 4.4.
-// Batches of four steps keep 4 KB a column block in flight a wave; a ring of three did not fit the registers of 4 waves a SIMD.
 template <int MT, int NC, int NW>
 __global__ __launch_bounds__(64 * NW) void mx_gemm_stream_kernel(MxGemmArgs p) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
@@ -297,6 +296,9 @@ __device__ __forceinline__ void buffer_to_lds4(__amdgpu_buffer_rsrc_t r, uint32_
 #endif
 }
 
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+
 struct TileParams {
   MxGemmArgs g;
   float *partial;   // [splits][M][N], or NULL
@@ -323,7 +325,7 @@ struct Piece {
 
 // Many rows.  Workgroups take pieces blockIdx, blockIdx + gridDim, .. and read them as one stream of steps through a ring in LDS:
 // the next piece's first steps arrive while the last ones of this are multiplied and its outputs stored.
-// 8191 x 4096 to 16384 with 256 x 256 tiles: 263 to 290 us, 3.8 to 4.2 PFLOP/s.  The matrix cores are busy 55% of the
+// 8191 x 4096 to 16384 with 256 x 256 tiles: 263 to 290 us by card, 3.8 to 4.2 PFLOP/s.  The matrix cores are busy 55% of the
 // time, at 1.8 GHz: under random codes the card lowers its clock (the instructions alone reach 5.9 PFLOP/s with them, 8.3
 // with zeros).  A step's reads of LDS take as long as its products, and a tile's outputs, staged and stored, 5 us of 34 in
 // which nothing is multiplied.  Measured and slower: weights straight to registers (308 us), steps of 128 channels, one
@@ -532,27 +534,32 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_gemm_tile_kernel(TileParams p
     const int eu = el >> 5, e32 = el & 31;
     const int rw = wm * 32 * TI, cw = wn * 32 * TJ;
     if constexpr (SPLIT) {
-      float *out = p.partial + (int64_t)cur.split * p.g.M * p.g.N;
+      const int left = cur.rows - rw - 4 * eu, n = cw + e32;
+      float *out = p.partial + ((int64_t)cur.split * p.g.M + cur.m0 + rw + 4 * eu) * p.g.N + cur.n0 + n;
 #pragma unroll
       for (int i = 0; i < TI; ++i) {
         pin(acc[i]);
 #pragma unroll
-        for (int j = 0; j < TJ; ++j)
+        for (int e = 0; e < 16; ++e) {
+          const int k = 32 * i + 8 * (e >> 2) + (e & 3);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int m = rw + 32 * i + 8 * (e >> 2) + 4 * eu + (e & 3), n = cw + 32 * j + e32;
-            if (m < cur.rows && n < cur.cols) out[(cur.m0 + m) * p.g.N + cur.n0 + n] = acc[i][j][e];
-          }
+          for (int j = 0; j < TJ; ++j)
+            if (k < left && n + 32 * j < cur.cols) out[k * p.g.N + 32 * j] = acc[i][j][e];
+        }
       }
     } else {
       // bf16 rows, 16 at a time, through the wave's own part of LDS, so that they leave in 16-byte pieces
-      constexpr int CPR = 4 * TJ;
+      constexpr int CPR = 4 * TJ, ROWS = 16 / TJ;  // pieces of a row, rows of 64 lanes
       uint8_t *stage = lds + STAGES * T::STAGE + wave * 16 * T::STRIDE;
+      uint8_t *to = stage + 4 * eu * T::STRIDE + e32 * 2;
+      const uint8_t *of = stage + el / CPR * T::STRIDE + el % CPR * 16;
+      const int n = cw + el % CPR * 8, left = n < cur.cols ? cur.rows - rw - el / CPR : 0;
+      uint16_t *out = p.g.y + (cur.m0 + rw + el / CPR) * p.g.ldy + cur.n0 + n;
       float bias[TJ];
 #pragma unroll
       for (int j = 0; j < TJ; ++j) {
-        const int n = cw + 32 * j + e32;
-        bias[j] = p.g.bias && n < cur.cols ? p.g.bias[cur.n0 + n] : 0.0f;
+        const int m = cw + 32 * j + e32;
+        bias[j] = p.g.bias && m < cur.cols ? p.g.bias[cur.n0 + m] : 0.0f;
       }
 #pragma unroll
       for (int i = 0; i < 2 * TI; ++i) {
@@ -562,17 +569,20 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_gemm_tile_kernel(TileParams p
 #pragma unroll
         for (int j = 0; j < TJ; ++j)
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            *reinterpret_cast<uint16_t *>(stage + (4 * eu) * T::STRIDE + e32 * 2 + (8 * (e >> 2) + (e & 3)) * T::STRIDE + 64 * j) =
-                (uint16_t)f32_to_bf16(acc[i / 2][j][8 * (i & 1) + e] + bias[j]);
+          for (int e = 0; e < 8; e += 2) {
+            v2f f{acc[i / 2][j][8 * (i & 1) + e], acc[i / 2][j][8 * (i & 1) + e + 1]};
+            f.x += bias[j];
+            f.y += bias[j];
+            const uint32_t two = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, v2bf));
+            uint8_t *at = to + (8 * (e >> 2) + (e & 3)) * T::STRIDE + 64 * j;
+            *reinterpret_cast<uint16_t *>(at) = (uint16_t)two;
+            *reinterpret_cast<uint16_t *>(at + T::STRIDE) = (uint16_t)(two >> 16);
+          }
         wave_lds_fence();
 #pragma unroll
-        for (int q = 0; q < CPR / 4; ++q) {
-          const int c = q * 64 + el, row = c / CPR, ch = c % CPR;
-          const int m = rw + 16 * i + row, n = cw + ch * 8;
-          if (m < cur.rows && n < cur.cols)
-            *reinterpret_cast<uint4 *>(p.g.y + (cur.m0 + m) * p.g.ldy + cur.n0 + n) =
-                *reinterpret_cast<const uint4 *>(stage + row * T::STRIDE + ch * 16);
+        for (int q = 0; q < TJ; ++q) {
+          const int k = 16 * i + q * ROWS;
+          if (k < left) *reinterpret_cast<uint4 *>(out + k * p.g.ldy) = *reinterpret_cast<const uint4 *>(of + q * ROWS * T::STRIDE);
         }
         wave_lds_fence();
       }
