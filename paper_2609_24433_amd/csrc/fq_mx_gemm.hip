@@ -667,24 +667,25 @@ hipError_t launch_tiles(const MxGemmArgs &g, int splits, float *ws, hipStream_t 
   return hipGetLastError();
 }
 
-// The kernels to choose from, and the microseconds that a call takes by what was measured (1400 drawn sizes of 1 to
+// The kernels to choose from, and the microseconds that a call takes by what was measured (2100 drawn sizes of 1 to
 // 8191 rows, K 128 to 32768, N 64 to 32768, each with every kernel and split, in a graph of calls in a row; the formulas are within
-// 7% (tiles) to 13% of a call at the root mean square, and the kernel that they choose takes 1.3% more than the best of all on
+// 7% (tiles) to 11% of a call at the root mean square, and the kernel that they choose takes 1.0% more than the best of all on
 // average, 48% at most, for calls of 3 us).
 struct StreamKind {
   int mt, nc, nw;
   hipError_t (*launch)(const MxGemmArgs &, hipStream_t);
-  // a call, a batch of a wave, a workgroup that a compute unit runs, and a step of 128 channels of all but its first
-  float call, batch, group, step;
+  // a call, a batch of a wave, a workgroup that a compute unit runs, a step of 128 channels of all but its first, and a
+  // million outputs
+  float call, batch, group, step, outputs;
 };
 const StreamKind kStream[] = {
-    {1, 1, 2, launch_stream<1, 1, 2>, 2.76f, 0.182f, 0.097f, 0.0248f},
-    {1, 1, 4, launch_stream<1, 1, 4>, 2.65f, 0.273f, 0.216f, 0.0244f},
-    {1, 2, 4, launch_stream<1, 2, 4>, 2.68f, 0.417f, 0.269f, 0.0356f},
-    {2, 1, 2, launch_stream<2, 1, 2>, 2.63f, 0.289f, 0.239f, 0.0365f},
-    {2, 2, 8, launch_stream<2, 2, 8>, 1.08f, 1.338f, 1.800f, 0.0541f},
-    {2, 4, 4, launch_stream<2, 4, 4>, 2.14f, 1.063f, 0.948f, 0.0733f},
-    {4, 4, 4, launch_stream<4, 4, 4>, 0.57f, 1.652f, 2.760f, 0.1325f},
+    {1, 1, 2, launch_stream<1, 1, 2>, 2.86f, 0.190f, 0.028f, 0.0243f, 1.12f},
+    {1, 1, 4, launch_stream<1, 1, 4>, 2.74f, 0.283f, 0.143f, 0.0239f, 1.19f},
+    {1, 2, 4, launch_stream<1, 2, 4>, 2.81f, 0.433f, 0.164f, 0.0353f, 0.82f},
+    {2, 1, 2, launch_stream<2, 1, 2>, 2.75f, 0.307f, 0.155f, 0.0353f, 0.76f},
+    {2, 2, 8, launch_stream<2, 2, 8>, 1.12f, 1.373f, 1.756f, 0.0521f, 0.35f},
+    {2, 4, 4, launch_stream<2, 4, 4>, 2.72f, 1.061f, 0.361f, 0.0734f, 1.16f},
+    {4, 4, 4, launch_stream<4, 4, 4>, 1.37f, 1.655f, 1.857f, 0.1291f, 1.06f},
 };
 struct TileKind {
   int bm, bn;
@@ -694,9 +695,9 @@ struct TileKind {
   float call, step, step_full, outputs, join, partial;
 };
 const TileKind kTiles[] = {
-    {64, 128, launch_tiles<1, 1, 2, 4, 4>, 3.97f, 0.398f, 0.017f, 1.53f, 3.18f, 0.229f},
-    {128, 128, launch_tiles<2, 1, 2, 4, 3>, 4.21f, 0.472f, 0.060f, 1.76f, 3.34f, 0.268f},
-    {128, 256, launch_tiles<2, 2, 2, 4, 2>, 5.07f, 0.769f, 0.142f, 2.76f, 3.60f, 0.263f},
+    {64, 128, launch_tiles<1, 1, 2, 4, 4>, 3.94f, 0.400f, 0.014f, 1.35f, 2.96f, 0.261f},
+    {128, 128, launch_tiles<2, 1, 2, 4, 3>, 4.16f, 0.479f, 0.050f, 1.43f, 3.21f, 0.297f},
+    {128, 256, launch_tiles<2, 2, 2, 4, 2>, 5.01f, 0.766f, 0.144f, 2.25f, 3.45f, 0.286f},
     {256, 256, launch_tiles<4, 2, 2, 4, 2>, 6.68f, 1.155f, 0.299f, 3.04f, 4.08f, 0.289f},
 };
 
@@ -720,7 +721,8 @@ MxPlan mx_plan(int64_t M, int64_t N, int64_t K) {
     if (groups * 64 * k.nw > 0xFFFFFFFF) continue;  // threads of a launch
     const float rounds = (float)((groups + kUnits - 1) / kUnits);
     const int batches = (ktot + 4 * k.nw - 1) / (4 * k.nw);
-    const float t = k.call + k.batch * (float)batches + rounds * k.group + (rounds - 1.0f) * (float)ktot * k.step;
+    const float t = k.call + k.batch * (float)batches + rounds * k.group + (rounds - 1.0f) * (float)ktot * k.step +
+                    k.outputs * 1e-6f * (float)M * (float)N;
     if (t < least) least = t, best = MxPlan{i, -1, 1, false};
   }
   for (int i = 0; i < (int)(sizeof kTiles / sizeof kTiles[0]); ++i) {
