@@ -314,6 +314,7 @@ struct TileShape {
   static constexpr int LDS = STAGES * STAGE + NW * 16 * STRIDE;
   static constexpr int IA = A / 1024 / NW, IB = B / 1024 / NW, IS_ALL = S / 256, IS = (IS_ALL + NW - 1) / NW;
   static constexpr int LPS = IA + IB + IS;
+  static constexpr int PER_UNIT = 163840 / LDS;  // workgroups of a compute unit
   static_assert(IA * NW * 1024 == A && IB * NW * 1024 == B && BM % 64 == 0 && BN % 64 == 0, "whole loads");
 };
 
@@ -331,6 +332,9 @@ struct Piece {
 // which nothing is multiplied.  Measured and slower: weights straight to registers (308 us), steps of 128 channels, one
 // or two workgroups a unit (321), outputs stored in pieces of 64 bytes from exchanged operands (313), four waves with tiles of
 // 128 x 128, and accumulators in ordinary registers (17%).
+// Tiles of 64 x 64 (four waves, two workgroups a unit) are for what fills the card with no more: 816 x 4096 to 1024 8.9 us (64 x
+// 128 10.5, 128 x 128 11.9), 1024 x 8192 to 1024 14.5 (17.3, 19.9); with two workgroups of 128 x 128 the larger shapes lose to
+// 256 x 256 all the same.
 template <int TI, int TJ, int WM, int WN, int STAGES, bool SPLIT>
 __global__ __launch_bounds__(64 * WM * WN) void mx_gemm_tile_kernel(TileParams p) {
   using T = TileShape<TI, TJ, WM, WN, STAGES>;
@@ -650,7 +654,8 @@ hipError_t launch_tile(TileParams p, hipStream_t s) {
   p.ntn = (int)((p.g.N + T::BN - 1) / T::BN);
   p.tiles = p.ntm * p.ntn;
   const int64_t total = (int64_t)p.tiles * p.splits;
-  hipLaunchKernelGGL((mx_gemm_tile_kernel<TI, TJ, WM, WN, STAGES, SPLIT>), dim3((unsigned)(total < kUnits ? total : kUnits)), dim3(64 * T::NW),
+  const int64_t most = kUnits * T::PER_UNIT;
+  hipLaunchKernelGGL((mx_gemm_tile_kernel<TI, TJ, WM, WN, STAGES, SPLIT>), dim3((unsigned)(total < most ? total : most)), dim3(64 * T::NW),
                      T::LDS, s, p);
   return hipGetLastError();
 }
@@ -667,9 +672,9 @@ hipError_t launch_tiles(const MxGemmArgs &g, int splits, float *ws, hipStream_t 
   return hipGetLastError();
 }
 
-// The kernels to choose from, and the microseconds that a call takes by what was measured (2100 drawn sizes of 1 to
+// The kernels to choose from, and the microseconds that a call takes by what was measured (1700 drawn sizes of 1 to
 // 8191 rows, K 128 to 32768, N 64 to 32768, each with every kernel and split, in a graph of calls in a row; the formulas are within
-// 7% (tiles) to 11% of a call at the root mean square, and the kernel that they choose takes 1.0% more than the best of all on
+// 7% (tiles) to 11% of a call at the root mean square, and the kernel that they choose takes 1.3% more than the best of all on
 // average, 48% at most, for calls of 3 us).
 struct StreamKind {
   int mt, nc, nw;
@@ -679,26 +684,26 @@ struct StreamKind {
   float call, batch, group, step, outputs;
 };
 const StreamKind kStream[] = {
-    {1, 1, 2, launch_stream<1, 1, 2>, 2.86f, 0.190f, 0.028f, 0.0243f, 1.12f},
-    {1, 1, 4, launch_stream<1, 1, 4>, 2.74f, 0.283f, 0.143f, 0.0239f, 1.19f},
-    {1, 2, 4, launch_stream<1, 2, 4>, 2.81f, 0.433f, 0.164f, 0.0353f, 0.82f},
-    {2, 1, 2, launch_stream<2, 1, 2>, 2.75f, 0.307f, 0.155f, 0.0353f, 0.76f},
-    {2, 2, 8, launch_stream<2, 2, 8>, 1.12f, 1.373f, 1.756f, 0.0521f, 0.35f},
-    {2, 4, 4, launch_stream<2, 4, 4>, 2.72f, 1.061f, 0.361f, 0.0734f, 1.16f},
-    {4, 4, 4, launch_stream<4, 4, 4>, 1.37f, 1.655f, 1.857f, 0.1291f, 1.06f},
+    {1, 1, 2, launch_stream<1, 1, 2>, 2.84f, 0.183f, 0.031f, 0.0245f, 1.07f},
+    {1, 1, 4, launch_stream<1, 1, 4>, 2.71f, 0.278f, 0.157f, 0.0241f, 0.97f},
+    {1, 2, 4, launch_stream<1, 2, 4>, 2.80f, 0.426f, 0.149f, 0.0354f, 0.95f},
+    {2, 1, 2, launch_stream<2, 1, 2>, 2.73f, 0.295f, 0.157f, 0.0358f, 0.75f},
+    {2, 2, 8, launch_stream<2, 2, 8>, 1.17f, 1.357f, 1.695f, 0.0527f, 0.57f},
+    {2, 4, 4, launch_stream<2, 4, 4>, 2.70f, 1.063f, 0.362f, 0.0733f, 1.17f},
+    {4, 4, 4, launch_stream<4, 4, 4>, 1.43f, 1.654f, 1.810f, 0.1296f, 1.09f},
 };
 struct TileKind {
-  int bm, bn;
+  int bm, bn, per_unit;
   hipError_t (*launch)(const MxGemmArgs &, int, float *, hipStream_t);
   // a call, a step of 256 channels alone and with all compute units at work, the outputs of a tile then; a split K's
   // second kernel, and a million bytes of partial sums
   float call, step, step_full, outputs, join, partial;
 };
 const TileKind kTiles[] = {
-    {64, 128, launch_tiles<1, 1, 2, 4, 4>, 3.94f, 0.400f, 0.014f, 1.35f, 2.96f, 0.261f},
-    {128, 128, launch_tiles<2, 1, 2, 4, 3>, 4.16f, 0.479f, 0.050f, 1.43f, 3.21f, 0.297f},
-    {128, 256, launch_tiles<2, 2, 2, 4, 2>, 5.01f, 0.766f, 0.144f, 2.25f, 3.45f, 0.286f},
-    {256, 256, launch_tiles<4, 2, 2, 4, 2>, 6.68f, 1.155f, 0.299f, 3.04f, 4.08f, 0.289f},
+    {64, 64, TileShape<1, 1, 2, 2, 3>::PER_UNIT, launch_tiles<1, 1, 2, 2, 3>, 3.50f, 0.299f, 0.109f, 1.54f, 3.05f, 0.189f},
+    {128, 128, TileShape<2, 1, 2, 4, 3>::PER_UNIT, launch_tiles<2, 1, 2, 4, 3>, 4.18f, 0.476f, 0.055f, 1.59f, 3.29f, 0.282f},
+    {128, 256, TileShape<2, 2, 2, 4, 2>::PER_UNIT, launch_tiles<2, 2, 2, 4, 2>, 5.03f, 0.767f, 0.143f, 2.51f, 3.55f, 0.274f},
+    {256, 256, TileShape<4, 2, 2, 4, 2>::PER_UNIT, launch_tiles<4, 2, 2, 4, 2>, 6.68f, 1.155f, 0.299f, 3.04f, 4.08f, 0.289f},
 };
 
 // One launch or two: the one rounds each batch of a wave before the product takes it, 1.2 us a batch, and pays up to three or
@@ -731,7 +736,8 @@ MxPlan mx_plan(int64_t M, int64_t N, int64_t K) {
       const int per = (steps + want - 1) / want, splits = (steps + per - 1) / per;  // no slice is empty
       const int64_t pieces = ((M + k.bm - 1) / k.bm) * ((N + k.bn - 1) / k.bn) * splits;
       if (pieces > 0x7FFFFFFF) continue;
-      const float rounds = (float)((pieces + kUnits - 1) / kUnits), full = (float)pieces / (rounds * (float)kUnits);
+      const int64_t units = kUnits * k.per_unit;
+      const float rounds = (float)((pieces + units - 1) / units), full = (float)pieces / (rounds * (float)units);
       float t = k.call + rounds * ((float)per * (k.step + k.step_full * full) + k.outputs * full);
       if (splits > 1) t += k.join + k.partial * (float)splits * (float)M * (float)N * 4e-6f;
       if (t < least) least = t, best = MxPlan{-1, i, splits, false};

@@ -118,12 +118,14 @@ def test_product(M, N, K):
     assert torch.equal(fq().mx_gemm(*args), out[:M, :N])  # the same bits again, into rows of another stride
 
 
-# every kernel and way of splitting K that the sizes choose: tiles of 64 x 128 to 256 x 256, one a workgroup and several, K
+# every kernel and way of splitting K that the sizes choose: tiles of 64 x 64 to 256 x 256, one a workgroup and several, K
 # ending inside a step, whole and in slices with a short last one
 @pytest.mark.parametrize("M,N,K", [(300, 512, 512), (513, 784, 1024), (1000, 272, 4096), (700, 2048, 384), (2049, 1040, 256),
                                    (260, 16384, 128), (816, 16384, 640), (2100, 8208, 384), (1500, 4112, 896), (4100, 4112, 1152),
                                    (300, 256, 16384), (520, 2048, 8320), (816, 2048, 16384), (390, 272, 32768), (260, 1024, 7552),
-                                   (3000, 16384, 2176), (129, 32768, 256), (1338, 64, 12032), (620, 752, 12928), (1100, 80, 32640)])
+                                   (3000, 16384, 2176), (129, 32768, 256), (1338, 64, 12032), (620, 752, 12928), (1100, 80, 32640),
+                                   (116, 1504, 2944), (240, 928, 8064), (287, 2112, 4736), (75, 5728, 1920), (344, 2320, 384), (704, 1600, 2688),
+                                   (1165, 176, 10368), (1113, 1872, 27264), (170, 5616, 28288)])
 def test_product_of_many_rows(M, N, K):
     flush(f"mx_gemm M={M} N={N} K={K}")
     a, sa = operands(M, K, M)
