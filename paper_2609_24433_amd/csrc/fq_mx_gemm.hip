@@ -81,7 +81,7 @@ __device__ __forceinline__ void join_waves(const v4f (&acc)[MT][NC], uint8_t *ld
 //   Rows go through the wave's own part of LDS: loaded in operand order (a lane a row) they come at 37 bytes a ns and compute
 //   unit, four lanes a row at 120.  Weights are packed in operand order.
 //   Weights are the left operand, so that a lane comes to hold four adjacent columns of one row.
-// Bound by the way of the weights and by the launch: one token 2048 to 16384 (18 MB) 3.6 us in a graph of calls, 5.0 TB/s; 16384
+// Bound by the way of the weights and by the launch: one token 2048 to 16384 (18 MB) 3.3 us in a graph of calls, 5.4 TB/s; 16384
 // to 2048 5.4; 50 rows of the same 6.1 (11.8 with rows loaded in operand order and a scale word a step); 48 rows 4096 to 4096 4.4.
 template <int MT, int NC, int NW>
 __global__ __launch_bounds__(64 * NW) void mx_gemm_stream_kernel(MxGemmArgs p) {

@@ -762,7 +762,7 @@ def _matrix(t: torch.Tensor, dtype, shape, name: str, dev: int) -> Tuple[int, in
 
 
 def _new(like: torch.Tensor, shape, dtype) -> torch.Tensor:
-    return like.new_empty(shape, dtype=dtype) if type(like) is torch.Tensor else torch.empty(shape, dtype=dtype, device=like.device)
+    return like.new_empty(*shape, dtype=dtype) if type(like) is torch.Tensor else torch.empty(shape, dtype=dtype, device=like.device)
 
 
 def _gpu_stream(dev: int) -> int:
