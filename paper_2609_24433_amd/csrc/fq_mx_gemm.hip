@@ -12,6 +12,10 @@ namespace {
 
 constexpr int kUnits = 256;  // compute units
 
+// Buffers of the loads below begin where a load's step begins and end where the array's part that a workgroup reads ends, and
+// no load has a scalar offset: the hardware compares a buffer's size with the vector offset only, and zeros come back for
+// whatever lies behind.
+
 // Steps of 256 channels, the last of which may have 128.
 inline int steps_of(int K) { return (K / kTileK + 1) / 2; }
 
@@ -119,17 +123,23 @@ __global__ __launch_bounds__(64 * NW) void mx_gemm_stream_kernel(MxGemmArgs p) {
   auto load = [&](Batch &b, int buf, int at) {
     // (a batch behind the wave's share is asked of empty buffers: no branch, so that every wait knows its count)
     const int k = __builtin_amdgcn_readfirstlane(at), on = k < k1 ? -1 : 0;
-    const __amdgpu_buffer_rsrc_t ar = buffer_of(a0, abytes & on), wr = buffer_of(w0, wbytes & on);
+    const __amdgpu_buffer_rsrc_t wr = buffer_of(w0 + k * 1024, (wbytes - k * 1024) & on);
+    __amdgpu_buffer_rsrc_t ar[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int off = min(k + s, ktot - 1) * 64;
+      ar[s] = buffer_of(a0 + off, (abytes - off) & on);
+    }
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
       for (int s = 0; s < 4; ++s)
-        buffer_to_lds16(ar, avoff + (uint32_t)t * 8u * (uint32_t)p.K, (uint32_t)min(k + s, ktot - 1) * 64u, mine + ((buf * MT + t) * 4 + s) * 1024);
+        buffer_to_lds16(ar[s], avoff + (uint32_t)t * 8u * (uint32_t)p.K, 0, mine + ((buf * MT + t) * 4 + s) * 1024);
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        b.w[c][i] = __builtin_amdgcn_raw_buffer_load_b128(wr, wvoff + i * 256u + (uint32_t)c * (uint32_t)ktot * 1024u, (uint32_t)k * 1024u, 0);
+        b.w[c][i] = __builtin_amdgcn_raw_buffer_load_b128(wr, wvoff + i * 256u + (uint32_t)c * (uint32_t)ktot * 1024u, 0, 0);
     const int64_t step = min(k + g, ktot - 1);
 #pragma unroll
     for (int c = 0; c < NC; ++c) b.sw[c] = sw[c][step * p.N];
@@ -200,7 +210,8 @@ __global__ __launch_bounds__(64 * NW) void mx_token_kernel(TokenParams p) {
   const int k0 = wave * per, k1 = min(k0 + per, ktot);
 
   const float4 bias = bias_of<NC>(p.g, n0, cols);
-  const __amdgpu_buffer_rsrc_t wr = buffer_of(p.g.w + n0 / 16 * ktot * 1024, cols / 16 * ktot * 1024);
+  const uint8_t *w0 = p.g.w + n0 / 16 * ktot * 1024;
+  const int wbytes = cols / 16 * ktot * 1024;
   const uint32_t wvoff = g * 1024u + r16 * 16u;
   const uint32_t *sw[NC];
 #pragma unroll
@@ -222,11 +233,12 @@ __global__ __launch_bounds__(64 * NW) void mx_token_kernel(TokenParams p) {
     load_chunk<uint16_t>(p.q.x, at + (int64_t)j * 16, a.x);
     if (p.q.pre) load_mult(p.q.pre, j, a.pre);
     if (p.q.post) load_mult(p.q.post, j, a.post);
+    const __amdgpu_buffer_rsrc_t wr = buffer_of(w0 + k * 1024, wbytes - k * 1024);
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        b.w[c][i] = __builtin_amdgcn_raw_buffer_load_b128(wr, wvoff + i * 256u + (uint32_t)c * (uint32_t)ktot * 1024u, (uint32_t)k * 1024u, 0);
+        b.w[c][i] = __builtin_amdgcn_raw_buffer_load_b128(wr, wvoff + i * 256u + (uint32_t)c * (uint32_t)ktot * 1024u, 0, 0);
 #pragma unroll
     for (int c = 0; c < NC; ++c) b.s[c] = sw[c][(int64_t)min(k + g, ktot - 1) * p.g.N];
   };
@@ -288,6 +300,7 @@ __device__ __forceinline__ v16f mfma_mx_32(const v4i &a, int sa, const v4i &b, i
 #endif
 }
 
+// 4 bytes per lane (lane l -> dst + 4 l).
 __device__ __forceinline__ void buffer_to_lds4(__amdgpu_buffer_rsrc_t r, uint32_t voff, void *dst) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)dst, 4, voff, 0, 0, 0);
@@ -374,18 +387,24 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_gemm_tile_kernel(TileParams p
   int from_lin = blockIdx.x, from_step = from.first, a_bytes, w_bytes;
   const uint8_t *from_a, *from_w, *from_sa, *from_sw;
   auto turn = [&] {
-    from_a = p.g.a + from.m0 * (K / 2);
-    from_w = p.g.w + from.n0 / 16 * ktot * 1024;
+    from_a = p.g.a + from.m0 * (K / 2) + from.first * 128;
+    from_w = p.g.w + from.n0 / 16 * ktot * 1024 + from.first * 2048;
     from_sa = p.g.a_scale + 2 * from.first * msteps + from.m0 * 4;
     from_sw = p.g.w_scale + 2 * from.first * nsteps + from.n0 * 4;
-    a_bytes = from.rows * (K / 2);
-    w_bytes = from.cols / 16 * ktot * 1024;
+    a_bytes = from.rows * (K / 2) - from.first * 128;
+    w_bytes = from.cols / 16 * ktot * 1024 - from.first * 2048;
   };
   turn();
   auto advance = [&] {
     from_sa += 2 * msteps;
     from_sw += 2 * nsteps;
-    if (++from_step < from.last) return;
+    if (++from_step < from.last) {
+      from_a += 128;
+      from_w += 2048;
+      a_bytes -= 128;
+      w_bytes -= 2048;
+      return;
+    }
     from_lin += gridDim.x;
     if (from_lin < total) {
       from = piece_of(from_lin);
@@ -398,12 +417,11 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_gemm_tile_kernel(TileParams p
   auto issue = [&](int slot, int q) {
     uint8_t *st = lds + slot * T::STAGE;
     if (q < T::IA) {
-      buffer_to_lds16(buffer_of(from_a, a_bytes), avoff[q & 1] + (uint32_t)(q >> 1) * 8u * (uint32_t)K, (uint32_t)from_step * 128u,
-                      st + (wave * T::IA + q) * 1024);
+      buffer_to_lds16(buffer_of(from_a, a_bytes), avoff[q & 1] + (uint32_t)(q >> 1) * 8u * (uint32_t)K, 0, st + (wave * T::IA + q) * 1024);
     } else if (q < T::IA + T::IB) {
       const int kb = wave * T::IB + q - T::IA;
-      buffer_to_lds16(buffer_of(from_w, w_bytes), lane16 + (uint32_t)(kb >> 1) * (uint32_t)ktot * 1024u + (kb & 1) * 1024u,
-                      (uint32_t)from_step * 2048u, st + T::A + kb * 1024);
+      buffer_to_lds16(buffer_of(from_w, w_bytes), lane16 + (uint32_t)(kb >> 1) * (uint32_t)ktot * 1024u + (kb & 1) * 1024u, 0,
+                      st + T::A + kb * 1024);
     } else {
       const int idx = min(wave * T::IS + q - T::IA - T::IB, T::IS_ALL - 1);
       const bool is_b = idx >= T::BM / 32;
