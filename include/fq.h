@@ -477,7 +477,8 @@ fq_status fq_norm_mx_quant(const void *x_bf16, int64_t ldx, const void *residual
                            const float *post_inv, int64_t M, int64_t K, int b, void *sum_out, int64_t ld_sum, void *codes,
                            void *scales, void *stream);
 
-/* values bf16 [M, ldv] = bf16_rne(code * delta[t]) of fq_fwht_quant's or fq_norm_quant's codes (bits 4 or 8). */
+/* values bf16 [M, ldv] = bf16_rne(fl32(code * delta[t])) of fq_fwht_quant's or fq_norm_quant's codes (bits 4 or 8): the fp32
+ * product, rounded again.  (Beside a tie of bf16 a single rounding of the exact product may give the other neighbour.) */
 fq_status fq_read_codes(const void *codes, const float *delta, int64_t M, int64_t K, int bits, void *values_bf16, int64_t ldv,
                         void *stream);
 

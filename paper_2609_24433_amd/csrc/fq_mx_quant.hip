@@ -17,7 +17,7 @@
 // 92 us, 5.1 TB/s; 816 x 2048 5.4 us.  One row of 2048 takes 4.2 us: the rows' way from memory, the sum over lanes and
 // waves (lane moves instead of the LDS crossbar, 4.5 us -> 4.2), fp64 division and root, the gain's way, the largest value.
 //
-// read: code times scale, one rounding to bf16 (microscaled values need none).  16383 x 4096 8-bit codes (201 MB) 35 us, 5.7
+// read: code times scale in fp32, rounded to bf16 (microscaled values are exact in it).  16383 x 4096 8-bit codes (201 MB) 35 us, 5.7
 // TB/s.
 #include "fq_codes.hpp"
 #include "fq_launch.hpp"

@@ -835,7 +835,8 @@ def _values_out(out: Optional[torch.Tensor], codes: torch.Tensor, M: int, K: int
 
 
 def read_codes(codes: torch.Tensor, delta: torch.Tensor, bits: int, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Codes of fwht_quant or norm_quant, uint8 [M, K*bits/8] with delta fp32 [M], as values bf16 [M, K]."""
+    """Codes of fwht_quant or norm_quant, uint8 [M, K*bits/8] with delta fp32 [M], as values bf16 [M, K]: the fp32 product
+    of code and delta, rounded."""
     if bits != 8 and bits != 4:
         raise ValueError("bits: 4 or 8")
     shape = codes.shape
