@@ -85,8 +85,9 @@ __device__ __forceinline__ void join_waves(const v4f (&acc)[MT][NC], uint8_t *ld
 //   Rows go through the wave's own part of LDS: loaded in operand order (a lane a row) they come at 37 bytes a ns and compute
 //   unit, four lanes a row at 120.  Weights are packed in operand order.
 //   Weights are the left operand, so that a lane comes to hold four adjacent columns of one row.
-// Bound by the way of the weights and by the launch: one token 2048 to 16384 (18 MB) 3.3 us in a graph of calls, 5.4 TB/s; 16384
-// to 2048 5.4; 50 rows of the same 6.1 (11.8 with rows loaded in operand order and a scale word a step); 48 rows 4096 to 4096 4.4.
+// Bound by the way of the weights and by the launch (2.2 us in a graph for the smallest product): one token 2048 to 16384 (18 MB)
+// 3.4 us in a graph of the same call, whose weights the caches hold, 3.7 in a trace of eager ones, 4.9 TB/s; 16384 to 2048 5.4; 50
+// rows of the same 6.3 (11.8 with rows loaded in operand order and a scale word a step); 48 rows 4096 to 4096 4.1.
 template <int MT, int NC, int NW>
 __global__ __launch_bounds__(64 * NW) void mx_gemm_stream_kernel(MxGemmArgs p) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
@@ -196,7 +197,7 @@ struct TokenParams {
 // One or two tokens from bf16: the streaming kernel with the rounding inside.  While a batch's weights are on their way, its
 // wave rounds the same channels of the rows (16 lanes a 256-channel piece, as mx_quant's kernel, so the codes are the same)
 // into its part of LDS.  Every workgroup rounds the rows anew, which at this height costs less than a launch: 2048 to 16384
-// 4.0 us in a graph and 6.0 to 6.4 as two launches, 1024 to 4096 3.2 and 4.7, 4096 to 4096 4.4 and 5.4.  (The next batch's
+// 4.1 us in a graph and 6.0 to 6.4 as two launches, 1024 to 4096 3.2 and 4.7, 4096 to 4096 4.3 and 5.4.  (The next batch's
 // rows and weights asked for ahead cost a single batch 0.2 to 0.6 us more and saved eight 0.9.)
 template <int NC, int NW>
 __global__ __launch_bounds__(64 * NW) void mx_token_kernel(TokenParams p) {
@@ -339,15 +340,16 @@ struct Piece {
 
 // Many rows.  Workgroups take pieces blockIdx, blockIdx + gridDim, .. and read them as one stream of steps through a ring in LDS:
 // the next piece's first steps arrive while the last ones of this are multiplied and its outputs stored.
-// 8191 x 4096 to 16384 with 256 x 256 tiles: 263 to 290 us by card, 3.8 to 4.2 PFLOP/s.  The matrix cores are busy 55% of the
+// 8191 x 4096 to 16384 with 256 x 256 tiles: 268 to 295 us by card, 3.7 to 4.1 PFLOP/s.  The matrix cores are busy 55% of the
 // time, at 1.8 GHz: under random codes the card lowers its clock (the instructions alone reach 5.9 PFLOP/s with them, 8.3
-// with zeros).  A step's reads of LDS take as long as its products, and a tile's outputs, staged and stored, 5 us of 34 in
-// which nothing is multiplied.  Measured and slower: weights straight to registers (308 us), steps of 128 channels, one
+// with zeros).  Of some 3100 cycles a step 2050 are a SIMD's products, and 1150 a unit's reads of LDS and stagings (SQ_LDS_IDX_ACTIVE,
+// without what loads write there); waves wait 29% of theirs.  A tile's outputs, staged and stored, are 5 us of 34 in which
+// nothing is multiplied.  Measured and slower: weights straight to registers (308 us), steps of 128 channels, one
 // or two workgroups a unit (321), outputs stored in pieces of 64 bytes from exchanged operands (313), four waves with tiles of
 // 128 x 128, and accumulators in ordinary registers (17%).
-// Tiles of 64 x 64 (four waves, two workgroups a unit) are for what fills the card with no more: 816 x 4096 to 1024 8.9 us (64 x
-// 128 10.5, 128 x 128 11.9), 1024 x 8192 to 1024 14.5 (17.3, 19.9); with two workgroups of 128 x 128 the larger shapes lose to
-// 256 x 256 all the same.
+// Tiles of 64 x 64 (four waves, two workgroups a unit) are for what fills the card with no more: 382 x 256 to 2496 4.3 us (128 x
+// 128 5.3), 2669 x 1280 to 320 5.7 (7.3), 816 x 2048 to 2048 8.8 (9.2); with two workgroups of 128 x 128 the larger shapes lose
+// to 256 x 256 all the same.
 template <int TI, int TJ, int WM, int WN, int STAGES, bool SPLIT>
 __global__ __launch_bounds__(64 * WM * WN) void mx_gemm_tile_kernel(TileParams p) {
   using T = TileShape<TI, TJ, WM, WN, STAGES>;
@@ -579,7 +581,7 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_gemm_tile_kernel(TileParams p
       uint16_t *out = p.g.y + (cur.m0 + rw + el / CPR) * p.g.ldy + cur.n0 + n;
       float bias[TJ];
 #pragma unroll
-      for (int j = 0; j < TJ; ++j) {
+      for (int j = 0; j < TJ; ++j) {  // (816 x 2048 to 16384 takes 23.1 us with a bias and without one)
         const int m = cw + 32 * j + e32;
         bias[j] = p.g.bias && m < cur.cols ? p.g.bias[cur.n0 + m] : 0.0f;
       }
@@ -691,9 +693,9 @@ hipError_t launch_tiles(const MxGemmArgs &g, int splits, float *ws, hipStream_t 
 }
 
 // The kernels to choose from, and the microseconds that a call takes by what was measured (1700 drawn sizes of 1 to
-// 8191 rows, K 128 to 32768, N 64 to 32768, each with every kernel and split, in a graph of calls in a row; the formulas are within
-// 7% (tiles) to 11% of a call at the root mean square, and the kernel that they choose takes 1.3% more than the best of all on
-// average, 48% at most, for calls of 3 us).
+// 8191 rows, K 128 to 32768, N 64 to 32768, each with every kernel and split, in a graph of calls in a row).  On 450 other sizes of
+// the same range the formulas are within 6 to 8% (tiles) and 8 to 11% of a call at the root mean square, and the kernel that they
+// choose takes 1.3% more than the best of all on average, 23% at most, for a call of 3 us (48% among the 1700).
 struct StreamKind {
   int mt, nc, nw;
   hipError_t (*launch)(const MxGemmArgs &, hipStream_t);

@@ -4,21 +4,26 @@
 // product one rounding), then per block of 32 channels the scale 2^e, e = floor(log2 max |u|) - 2, and
 // the nearest E2M1 value of u 2^-e.  No reduction is wider than a block, so rows are not looked
 // at: threads take 16-channel chunks of all rows in a row, and a b-block is b / 16 lanes of a
-// 16-lane group, as in the prologue.  Bound by memory: 4095 x 16384 bf16 (170 MB) 32 us, 5.3 TB/s, what a large
-// copy reaches; 38 us with one fold and 43 with both, which every row reads again from the L2, 4 bytes a channel to its own 2.5
-// (two rows a thread share them: 37 and 39 us, but 5 to 10% more for every call under 30 us, and four rows are slower
-// still).  16384 x 2048 fp32 26 us, 5.9 TB/s.  50 x 1024 takes 3.4 us, a launch and one way to memory and back.
+// 16-lane group, as in the prologue.  Bound by memory and by the vector unit alike: 4095 x 16384 bf16 (170 MB) takes 32 us in a
+// graph with b = 128, 5.4 TB/s, what a large copy reaches, but 26 us without a rotation (caches hold part of such a repeated
+// call's rows); a wave issues 362 vector instructions for 16 channels a lane (SQ_INSTS_VALU), a SIMD one in 3.1 of its busy cycles.
+// One fold 39 us and both 42 (a trace of eager calls: 37, 44, 58): 17 instructions each, and most of it waiting (a wave's cycles grow
+// by 25% and 73%, all and three quarters of that in SQ_WAIT_ANY), since every row reads them again from the L2, 4 bytes a channel
+// to its own 2.5.
+// Two rows a thread share the folds, 1 to 4 us less, but take 5 to 10% more for every call under 30 us, and four rows are slower
+// still.  16384 x 2048 fp32 25 us, 6.2 TB/s.  50 x 1024 takes 2.7 us, of which a launch with a load and a store is 2.2.
 //
 // norm: h = bf16(x + r); s = 1 / sqrt(mean h^2 + eps) with the sum and the root in fp64 (a bf16's
 // square is exact there and the sum all but exact, so s does not depend on the order and the codes can
 // be reproduced bit for bit; in fp32 every order gives other last bits, and other codes next to a
 // tie); y = (h s) w; then the prologue's transform and rounding, or mx_quant's.  A row stays in
 // registers between its two reductions, so it is read once.  Bound by memory: 16383 x 4096 to 8 bits with a residual (470 MB)
-// 92 us, 5.1 TB/s; 816 x 2048 5.4 us.  One row of 2048 takes 4.2 us: the rows' way from memory, the sum over lanes and
-// waves (lane moves instead of the LDS crossbar, 4.5 us -> 4.2), fp64 division and root, the gain's way, the largest value.
+// 89 us in a graph, 5.3 TB/s (to 4 bits 85, microscaled 88); 816 x 2048 5.4 us, 50 x 1024 3.7.  One row of 2048 takes 3.7 us: the
+// rows' way from memory, the sum over lanes and waves (lane moves instead of the LDS crossbar, 0.3 us), fp64 division and root, the
+// gain's way, the largest value.
 //
-// read: code times scale in fp32, rounded to bf16 (microscaled values are exact in it).  16383 x 4096 8-bit codes (201 MB) 35 us, 5.7
-// TB/s.
+// read: code times scale in fp32, rounded to bf16 (microscaled values are exact in it).  16383 x 4096 8-bit codes (201 MB) 32 us in
+// a graph, 6.3 TB/s, 35 after the norm that wrote them; microscaled 4095 x 16384 (170 MB) 27 us, 6.3 TB/s.
 #include "fq_codes.hpp"
 #include "fq_launch.hpp"
 #include "fq_mx.hpp"
@@ -331,7 +336,8 @@ __global__ __launch_bounds__(kQuantThreads) void read_codes_kernel(ReadParams p)
 
 // ---------------- packing of weights ----------------
 
-// Tile (nb, kt) of 16 x 128 nibbles: lane l of a wave owns channel l % 16 and the block l / 16, 16 bytes.
+// Tile (nb, kt) of 16 x 128 nibbles: lane l of a wave owns channel l % 16 and the block l / 16, 16 bytes.  Once a weight: 16384 x
+// 2048 (17 MB each way) 6 us, 16384 x 16384 39 us, 6.9 TB/s (with caches), either way.
 __global__ __launch_bounds__(256) void mx_pack_kernel(const uint4 *from, int64_t pieces, int ktot, int unpack, uint4 *to) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
     const int64_t tile = i >> 6;
